@@ -442,6 +442,72 @@ rl_status rl_token_logprobs_static(void* cuda_stream, const void* H, int64_t ldH
                                    int64_t T, int64_t d, int64_t V,
                                    float* logp, float* entropy, float* lse, int32_t* dev_status);
 
+/* Supervised loss on the same head: softmax cross entropy of the targets with its gradients, for the warm start before the RL
+ * stage, a supervised term beside the policy loss, or (dH and dW NULL) an evaluation.  With z = W h_t, lse_t = log sum_j exp z_tj:
+ *   l_t  = (1 - e) (lse_t - z_ty) + e (lse_t - mean_j z_tj) + z_coef lse_t^2,   e = label_smoothing,   loss = sum_t w_t l_t,
+ *   dloss/dz_tj = w_t [(1 + 2 z_coef lse_t) p_tj - (1 - e) 1[j = y_t] - e / V],
+ * w_t = mask_t / sum(mask) unless opts say otherwise.  targets[T] int32 (rows with mask 0 are left out whatever they hold, and get 0
+ * in every output); everything else as in rl_policy_loss_fwd_bwd.  dH or dW may be NULL: a gradient nobody needs (a frozen trunk or a
+ * frozen head) is not formed.  dW is [V,d] fp32 or bf16, dH [T,d] bf16 or fp32.  Logits exist for one bounded slab of rows at a time,
+ * in fp32 (rl_set_slab_limits).  Workspace: rl_workspace_bytes_ce (a bf16 dW of a call of several slabs is added up in fp32);
+ * with neither gradient rl_workspace_bytes_logprobs.
+ * H may be stored in 8 bits (rl_quantize_rows): opts->H_scale[T] then holds the scales, H points to int8_t, ldH counts bytes and is a
+ * multiple of 16; the rows stand for bf16(H_scale[t] * H[t,k]) and dH is the gradient of those.
+ * Errors: label_smoothing outside [0, 1), z_coef negative or not finite, an unknown type, a bf16 dW with accumulate_dW or with a
+ * rl_dw_slab_hook set, NULL loss, W or (T > 0) H, targets -> RL_ERR_INVALID_ARG; shape / alignment / workspace as above. */
+typedef enum { RL_BF16 = 0, RL_FP32 = 1, RL_FP16 = 2 } rl_dtype;
+typedef struct {
+  size_t struct_size;         /* sizeof(rl_ce_opts); the rest zero unless set (dW_dtype: RL_FP32)  */
+  float label_smoothing;      /* e, in [0, 1)                                                  */
+  float z_coef;               /* >= 0                                                          */
+  const float* token_weight;  /* [T] or NULL: w_t = mask_t token_weight[t]                     */
+  const int64_t* token_count; /* device scalar or NULL: divisor of the token mean              */
+  int accumulate_dW;          /* non-zero: dW += gradient (fp32 dW)                            */
+  int dH_dtype, dW_dtype;     /* RL_BF16 or RL_FP32                                            */
+  const float* H_scale;       /* [T] or NULL: H is stored in 8 bits                            */
+  float* logp_out;            /* [T] or NULL: z_ty - lse_t                                     */
+  float* lse_out;             /* [T] or NULL                                                   */
+  float* token_loss_out;      /* [T] or NULL: l_t                                              */
+  float* metrics_out;         /* [8] or NULL: sums with w_t of lse - z_y, of lse - mean z, of  */
+                              /* lse^2, of 1[z_y is the row's largest], of lse; largest        */
+                              /* lse - z_y; number of rows that count; reserved                */
+} rl_ce_opts;
+rl_status rl_workspace_bytes_ce(rl_ctx* ctx, int64_t T, int64_t d, int64_t V, int dW_dtype, size_t* bytes);
+rl_status rl_cross_entropy_fwd_bwd(rl_ctx* ctx, const void* H, int64_t ldH, const void* W, int64_t ldW,
+                                   const int32_t* targets, const uint8_t* mask, int64_t T, int64_t d, int64_t V,
+                                   float* loss, void* dH, void* dW, const rl_ce_opts* opts);
+
+/* Rows in 8 bits, one scale each: for a head held in 8-bit integers (rows of W are channels), for the tokens that meet it, and for
+ * hidden states kept in 8 bits between the pass that makes them and the backward pass that uses them.
+ *   scale[r] = m / 127 and Q[r,k] = rint(X[r,k] * (127 / m)), half to even, m = max_k |X[r,k]|,
+ * both quotients rounded to fp32, the product not rounded before rint; X[r,k] is then about scale[r] * Q[r,k].  A row with m < 2^-100
+ * becomes zeros with scale 0, a row that holds an infinity or a NaN zeros with scale NaN (all that it enters is NaN).
+ * X: x_dtype, row stride ldX elements, any alignment (16-byte aligned rows are read faster).  Q: 16-byte aligned, ldQ a multiple of
+ * 16; bytes of a row from d on are left alone.  Needs no workspace.  rows = 0 is not an error.
+ * Errors: unknown type, NULL pointers -> RL_ERR_INVALID_ARG; ldX or ldQ < d -> RL_ERR_SHAPE; RL_ERR_ALIGNMENT. */
+rl_status rl_quantize_rows(rl_ctx* ctx, const void* X, int x_dtype, int64_t ldX, int64_t rows, int64_t d, int8_t* Q, int64_t ldQ,
+                           float* scale);
+
+/* Product of 8-bit rows: C[t,v] = a_scale[t] b_scale[v] sum_k A[t,k] B[v,k], in bf16, fp32 or fp16.  The sums are exact; they are
+ * rounded to fp32, multiplied by a_scale[t], then by b_scale[v], then rounded to C's type.  rl_int8_linear quantises the rows of X
+ * (rl_quantize_rows) into the workspace (rl_workspace_bytes_int8_linear) first: the logits of hidden states under a head held in 8
+ * bits.  A, B: 16-byte aligned, row strides multiples of 16 (the 16-byte words that a row's last elements lie in are read whole);
+ * d < 2^17, any number.  b_scale 16-byte aligned.  C: row stride ldC >= V elements, what lies between V and ldC is left alone;
+ * rows that start and end on 16 bytes are written faster.  Up to eight tokens are a stream of B, more run on the tensor cores.  T = 0 is not an error.
+ * Errors: unknown type, NULL pointers -> RL_ERR_INVALID_ARG; RL_ERR_SHAPE; RL_ERR_ALIGNMENT; RL_ERR_WORKSPACE (rl_int8_linear). */
+rl_status rl_int8_matmul(rl_ctx* ctx, const int8_t* A, int64_t ldA, const float* a_scale, const int8_t* B, int64_t ldB,
+                         const float* b_scale, int64_t T, int64_t d, int64_t V, void* C, int c_dtype, int64_t ldC);
+rl_status rl_workspace_bytes_int8_linear(rl_ctx* ctx, int64_t T, int64_t d, size_t* bytes);
+rl_status rl_int8_linear(rl_ctx* ctx, const void* X, int x_dtype, int64_t ldX, const int8_t* B, int64_t ldB, const float* b_scale,
+                         int64_t T, int64_t d, int64_t V, void* C, int c_dtype, int64_t ldC);
+
+/* rl_token_logprobs under a head held in 8 bits: W [V,d] int8_t with w_scale[V] (16-byte aligned), ldW a multiple of 16; the valid rows
+ * of H (bf16) are quantised as they are compacted.  Logits are those of rl_int8_linear before their last rounding and are not
+ * kept.  Twice the tensor throughput and half the bytes of W.  Workspace: rl_workspace_bytes_logprobs. */
+rl_status rl_token_logprobs_int8(rl_ctx* ctx, const void* H, int64_t ldH, const int8_t* W, int64_t ldW, const float* w_scale,
+                                 const int32_t* tokens, const uint8_t* mask, int64_t T, int64_t d, int64_t V,
+                                 float* logp, float* entropy, float* lse);
+
 /* Instrumentation.  rl_launch_count: kernels this context has launched so far.
  * rl_set_profiling(on): when on, every kernel (or group of small kernels) is bracketed by a pair of CUDA events
  * on the context's stream (at most 65536 launch groups are kept between two reads; later ones go untimed).

@@ -40,3 +40,30 @@ def fused_grpo_head_loss(H, W, tokens, old_logp, ref_logp, adv, mask, eps_low=0.
     """
     return _FusedHeadLoss.apply(H, W, tokens, old_logp, ref_logp, adv, mask, eps_low, eps_high, beta, ent_coef,
                                 token_weight, agg_mode, sequence_level, seq_offsets)
+
+
+class _FusedCrossEntropy(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, H, W, targets, mask, label_smoothing, z_coef, token_weight, token_count, want_dH, want_dW):
+        lib = default_context(W.device.index or 0)
+        out = lib.rl_cross_entropy_fwd_bwd(H.detach(), W.detach(), targets, mask, label_smoothing=label_smoothing, z_coef=z_coef,
+                                           token_weight=token_weight, token_count=token_count, want_dH=want_dH, want_dW=want_dW,
+                                           dW_bf16=True)
+        ctx.save_for_backward(out.get("dH"), out.get("dW"))
+        ctx.mark_non_differentiable(out["logp"])
+        return out["loss"].reshape(()).clone(), out["logp"]
+
+    @staticmethod
+    def backward(ctx, g_loss, *_):
+        dH, dW = ctx.saved_tensors
+        return (None if dH is None else dH * g_loss, None if dW is None else dW * g_loss) + (None,) * 8
+
+
+def fused_cross_entropy(H, W, targets, mask=None, label_smoothing=0.0, z_coef=0.0, token_weight=None, token_count=None):
+    """Supervised loss of `targets` as a differentiable scalar in H [T,d] bf16 and W [V,d] bf16: (loss, logp[T]).
+
+    Gradients (bf16) are formed with the loss, for those of H and W that ask for one.
+    """
+    grad = torch.is_grad_enabled()
+    return _FusedCrossEntropy.apply(H, W, targets, mask, label_smoothing, z_coef, token_weight, token_count,
+                                    grad and H.requires_grad, grad and W.requires_grad)

@@ -56,6 +56,25 @@ class rl_loss_opts(ctypes.Structure):
         ("token_count", c_void_p),
     ]
 
+
+class rl_ce_opts(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", c_size_t),
+        ("label_smoothing", c_float),
+        ("z_coef", c_float),
+        ("token_weight", c_void_p),
+        ("token_count", c_void_p),
+        ("accumulate_dW", c_int),
+        ("dH_dtype", c_int),
+        ("dW_dtype", c_int),
+        ("H_scale", c_void_p),
+        ("logp_out", c_void_p),
+        ("lse_out", c_void_p),
+        ("token_loss_out", c_void_p),
+        ("metrics_out", c_void_p),
+    ]
+
+
 DW_SLAB_HOOK = ctypes.CFUNCTYPE(None, c_void_p, c_int, c_int64, c_int64)
 
 
@@ -153,12 +172,20 @@ def load_library():
                                              c_int64, c_int64, P, P, P, c_float, c_float, c_float, P, P, P,
                                              POINTER(rl_loss_opts)]
     lib.rl_policy_loss_shard_bwd.restype = c_int
+    lib.rl_workspace_bytes_ce.argtypes = [P, c_int64, c_int64, c_int64, c_int, POINTER(c_size_t)]
+    lib.rl_cross_entropy_fwd_bwd.argtypes = [P, P, c_int64, P, c_int64, P, P, c_int64, c_int64, c_int64, P, P, P, POINTER(rl_ce_opts)]
+    lib.rl_quantize_rows.argtypes = [P, P, c_int, c_int64, c_int64, c_int64, P, c_int64, P]
+    lib.rl_int8_matmul.argtypes = [P, P, c_int64, P, P, c_int64, P, c_int64, c_int64, c_int64, P, c_int, c_int64]
+    lib.rl_workspace_bytes_int8_linear.argtypes = [P, c_int64, c_int64, POINTER(c_size_t)]
+    lib.rl_int8_linear.argtypes = [P, P, c_int, c_int64, P, c_int64, P, c_int64, c_int64, c_int64, P, c_int, c_int64]
+    lib.rl_token_logprobs_int8.argtypes = [P, P, c_int64, P, c_int64, P, P, P, c_int64, c_int64, c_int64, P, P, P]
     for name in ("rl_create", "rl_destroy", "rl_set_stream", "rl_workspace_bytes", "rl_workspace_bytes_host",
                  "rl_workspace_bytes_kl", "rl_workspace_bytes_logprobs",
                  "rl_set_workspace", "rl_set_slab_limits", "rl_last_device_status", "rl_grpo_advantages", "rl_grpo_advantages_ex",
                  "rl_token_logprobs", "rl_policy_loss_fwd_bwd", "rl_policy_loss_fwd_bwd_ex",
                  "rl_policy_loss_fwd_bwd_host", "rl_selftest_gemm", "rl_launch_count", "rl_set_profiling",
-                 "rl_profile_read"):
+                 "rl_profile_read", "rl_workspace_bytes_ce", "rl_cross_entropy_fwd_bwd", "rl_quantize_rows", "rl_int8_matmul",
+                 "rl_workspace_bytes_int8_linear", "rl_int8_linear", "rl_token_logprobs_int8"):
         getattr(lib, name).restype = c_int
     _load_host_calls(lib)
     _lib = lib   # last: whoever finds it finds the host half too
@@ -218,6 +245,26 @@ def _check_array(x, n, dtype=torch.float32):
 def _check_rows(T, tokens, mask):
     _check_array(tokens, T, torch.int32)
     assert mask is None or (mask.element_size() == 1 and mask.is_contiguous() and mask.numel() >= T)
+
+
+def _check_here(device, *tensors):
+    """Every tensor (None: not given) lies on the context's device."""
+    for x in tensors:
+        assert x is None or x.device == device, f"tensor on {x.device}, context on {device}"
+
+
+DTYPES = {torch.bfloat16: 0, torch.float32: 1, torch.float16: 2}   # rl_dtype
+
+
+def _row_stride(x):
+    """Row stride of a matrix whose rows are contiguous; of a single row (or none) its length."""
+    assert x.dim() == 2 and (x.stride(1) == 1 or x.shape[1] == 1)
+    return x.stride(0) if x.shape[0] > 1 else x.shape[1]
+
+
+def _row_stride_i8(x):
+    """The same of 8-bit rows, which start on multiples of 16 bytes."""
+    return _row_stride(x) if x.shape[0] > 1 else (x.shape[1] + 15) // 16 * 16
 
 
 def _check(status, where):
@@ -447,6 +494,125 @@ class Context:
                 opts.kl_out = out["kl"].data_ptr()
         _check(self.lib.rl_policy_loss_fwd_bwd_ex(*args, byref(opts)), "rl_policy_loss_fwd_bwd_ex")
         return out
+
+    # ------------------------------------------------------------------ supervised loss
+    def rl_cross_entropy_fwd_bwd(self, H, W, targets, mask=None, label_smoothing=0.0, z_coef=0.0, token_weight=None, token_count=None,
+                                 H_scale=None, want_dH=True, want_dW=True, dW_bf16=False, dH_fp32=False, accumulate_dW=False,
+                                 loss=None, dH=None, dW=None):
+        """Softmax cross entropy of `targets` [T] int32 and its gradients: dict(loss [1], dH [T, d], dW [V, d], logp [T], lse [T],
+        token_loss [T], metrics [8]); a gradient that is not wanted is not formed and left out.  H [T, d] is bf16, or int8 with H_scale
+        [T] (rl_quantize_rows); dH is the gradient of what that stands for."""
+        self._bind_stream()
+        T, d = H.shape
+        V = W.shape[0]
+        assert W.dtype == torch.bfloat16 and W.dim() == 2 and W.shape[1] == d and W.stride(1) == 1
+        assert H.dtype == (torch.bfloat16 if H_scale is None else torch.int8) and H.stride(1) == 1
+        _check_here(self.device, H, W, targets, mask, token_weight, token_count, H_scale, loss, dH, dW)
+        _check_rows(T, targets, mask)
+        _check_array(token_weight, T)
+        _check_array(H_scale, T)
+        _check_array(loss, 1)
+        assert token_count is None or (token_count.dtype == torch.int64 and token_count.numel() == 1)
+        dH_type = torch.float32 if dH_fp32 else torch.bfloat16
+        dW_type = torch.bfloat16 if dW_bf16 else torch.float32
+        _check_array(dH, T * d, dH_type)
+        _check_array(dW, V * d, dW_type)
+        assert not (accumulate_dW and dW is None), "accumulate_dW adds to a dW that is given"
+        need = c_size_t()
+        if want_dH or want_dW or T == 0:
+            _check(self.lib.rl_workspace_bytes_ce(self.handle, T, d, V, DTYPES[dW_type if want_dW else torch.float32], byref(need)),
+                   "rl_workspace_bytes_ce")
+        else:
+            _check(self.lib.rl_workspace_bytes_logprobs(self.handle, T, d, V, byref(need)), "rl_workspace_bytes_logprobs")
+        self._need_workspace(need.value)
+        dev = W.device
+        out = dict(loss=torch.empty(1, dtype=torch.float32, device=dev) if loss is None else loss)
+        if want_dH:
+            out["dH"] = torch.empty(T, d, dtype=dH_type, device=dev) if dH is None else dH
+        if want_dW:
+            out["dW"] = torch.empty(V, d, dtype=dW_type, device=dev) if dW is None else dW
+        out["logp"], out["lse"], out["token_loss"] = (torch.empty(T, dtype=torch.float32, device=dev) for _ in range(3))
+        out["metrics"] = torch.empty(8, dtype=torch.float32, device=dev)
+        opts = rl_ce_opts(ctypes.sizeof(rl_ce_opts), label_smoothing, z_coef, _ptr(token_weight), _ptr(token_count), int(accumulate_dW),
+                          DTYPES[dH_type], DTYPES[dW_type], _ptr(H_scale), _ptr(out["logp"]), _ptr(out["lse"]),
+                          _ptr(out["token_loss"]), _ptr(out["metrics"]))
+        _check(self.lib.rl_cross_entropy_fwd_bwd(
+            self.handle, _ptr(H), _row_stride(H) if H_scale is None else _row_stride_i8(H), _ptr(W), _row_stride(W), _ptr(targets),
+            _ptr(mask), T, d, V, _ptr(out["loss"]), _ptr(out.get("dH")), _ptr(out.get("dW")), byref(opts)), "rl_cross_entropy_fwd_bwd")
+        return out
+
+    def _need_workspace(self, nbytes):
+        if self._ws is None or self._ws.numel() < nbytes:
+            self._ws = None
+            self._ws = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=self.device)
+        _check(self.lib.rl_set_workspace(self.handle, _ptr(self._ws), self._ws.numel()), "rl_set_workspace")
+
+    # ------------------------------------------------------------------ 8-bit rows
+    def rl_quantize_rows(self, X, Q=None, scale=None):
+        """Rows of X [N, d] (bf16, fp16 or fp32) in 8 bits: (Q [N, d] int8 whose rows start on multiples of 16 bytes, scale [N] fp32)."""
+        self._bind_stream()
+        N, d = X.shape
+        if Q is None:
+            Q = torch.empty(N, (d + 15) // 16 * 16, dtype=torch.int8, device=X.device)[:, :d]
+        if scale is None:
+            scale = torch.empty(N, dtype=torch.float32, device=X.device)
+        _check_here(self.device, X, Q, scale)
+        _check_array(scale, N)
+        assert Q.dtype == torch.int8 and Q.shape == X.shape
+        _check(self.lib.rl_quantize_rows(self.handle, _ptr(X), DTYPES[X.dtype], _row_stride(X), N, d, _ptr(Q), _row_stride_i8(Q),
+                                         _ptr(scale)), "rl_quantize_rows")
+        return Q, scale
+
+    def _int8_out(self, T, Wq, w_scale, out_dtype, out):
+        V = Wq.shape[0]
+        assert Wq.dtype == torch.int8
+        _check_array(w_scale, V)
+        if out is None:
+            out = torch.empty(T, V, dtype=out_dtype, device=Wq.device)
+        assert out.shape == (T, V) and out.dtype == out_dtype
+        return out
+
+    def rl_int8_matmul(self, A, a_scale, Wq, w_scale, out_dtype=torch.bfloat16, out=None):
+        """[T, V] = a_scale[t] w_scale[v] sum_k A[t, k] Wq[v, k] of 8-bit rows (rl_quantize_rows)."""
+        self._bind_stream()
+        T, d = A.shape
+        assert A.dtype == torch.int8 and Wq.shape[1] == d
+        _check_array(a_scale, T)
+        out = self._int8_out(T, Wq, w_scale, out_dtype, out)
+        _check_here(self.device, A, a_scale, Wq, w_scale, out)
+        _check(self.lib.rl_int8_matmul(self.handle, _ptr(A), _row_stride_i8(A), _ptr(a_scale), _ptr(Wq), _row_stride_i8(Wq), _ptr(w_scale),
+                                       T, d, Wq.shape[0], _ptr(out), DTYPES[out_dtype], _row_stride(out)), "rl_int8_matmul")
+        return out
+
+    def rl_int8_linear(self, X, Wq, w_scale, out_dtype=torch.bfloat16, out=None):
+        """Logits [T, V] of hidden states X [T, d] (bf16, fp16 or fp32) under a head held in 8 bits: Wq [V, d] int8, w_scale [V]."""
+        self._bind_stream()
+        T, d = X.shape
+        assert Wq.shape[1] == d
+        out = self._int8_out(T, Wq, w_scale, out_dtype, out)
+        _check_here(self.device, X, Wq, w_scale, out)
+        need = c_size_t()
+        _check(self.lib.rl_workspace_bytes_int8_linear(self.handle, T, d, byref(need)), "rl_workspace_bytes_int8_linear")
+        self._need_workspace(need.value)
+        _check(self.lib.rl_int8_linear(self.handle, _ptr(X), DTYPES[X.dtype], _row_stride(X), _ptr(Wq), _row_stride_i8(Wq), _ptr(w_scale),
+                                       T, d, Wq.shape[0], _ptr(out), DTYPES[out_dtype], _row_stride(out)), "rl_int8_linear")
+        return out
+
+    def rl_token_logprobs_int8(self, H, Wq, w_scale, tokens, mask=None):
+        """rl_token_logprobs under a head held in 8 bits: (logp, entropy, lse), each [T]."""
+        self._bind_stream()
+        T, d = H.shape
+        V = Wq.shape[0]
+        assert H.dtype == torch.bfloat16 and Wq.dtype == torch.int8 and Wq.shape[1] == d
+        _check_here(self.device, H, Wq, w_scale, tokens, mask)
+        _check_array(w_scale, V)
+        _check_rows(T, tokens, mask)
+        self.ensure_workspace(T, d, V, scoring=True)
+        logp, ent, lse = (torch.empty(T, dtype=torch.float32, device=H.device) for _ in range(3))
+        _check(self.lib.rl_token_logprobs_int8(self.handle, _ptr(H), _row_stride(H), _ptr(Wq), _row_stride_i8(Wq), _ptr(w_scale),
+                                               _ptr(tokens), _ptr(mask), T, d, V, _ptr(logp), _ptr(ent), _ptr(lse)),
+               "rl_token_logprobs_int8")
+        return logp, ent, lse
 
     KL_ESTIMATES = {"k1": 0, "k3": 1, "given": 2}
 
@@ -761,6 +927,26 @@ def rl_token_logprobs(H, W, tokens, mask=None):
 def rl_policy_loss_fwd_bwd(H, W, tokens, old_logp, ref_logp, adv, mask, eps_low, eps_high, beta, **kw):
     return default_context(W.device.index or 0).rl_policy_loss_fwd_bwd(
         H, W, tokens, old_logp, ref_logp, adv, mask, eps_low, eps_high, beta, **kw)
+
+
+def rl_cross_entropy_fwd_bwd(H, W, targets, mask=None, **kw):
+    return default_context(W.device.index or 0).rl_cross_entropy_fwd_bwd(H, W, targets, mask, **kw)
+
+
+def rl_quantize_rows(X, **kw):
+    return default_context(X.device.index or 0).rl_quantize_rows(X, **kw)
+
+
+def rl_int8_matmul(A, a_scale, Wq, w_scale, **kw):
+    return default_context(Wq.device.index or 0).rl_int8_matmul(A, a_scale, Wq, w_scale, **kw)
+
+
+def rl_int8_linear(X, Wq, w_scale, **kw):
+    return default_context(Wq.device.index or 0).rl_int8_linear(X, Wq, w_scale, **kw)
+
+
+def rl_token_logprobs_int8(H, Wq, w_scale, tokens, mask=None):
+    return default_context(Wq.device.index or 0).rl_token_logprobs_int8(H, Wq, w_scale, tokens, mask)
 
 
 def rl_token_logprobs_static(H, W, tokens, mask, logp, entropy=None, lse=None, dev_status=None):

@@ -22,10 +22,12 @@ __device__ __forceinline__ float ex2_approx(float x) {
 // Forward statistics (policy over the vocabulary, section 2.2): for its row and the vocabulary
 // range of the work unit, keeps the running maximum M, S = sum exp(z-M), A = sum exp(z-M) z and
 // the logit of the sampled token.  Logits never leave the chip; one float4 per (range, row) does.
-struct RowStats {
+// SUM: A = sum z instead, for the cross entropy, whose smoothed labels ask for the mean logit and which needs no entropy.
+template <bool SUM>
+struct RowStatsOf {
   static constexpr bool kParts = false;
   static constexpr int kSideWarps = 0;
-  static constexpr bool kFeeds = false, kAhead = false;
+  static constexpr bool kFeeds = false, kAhead = false, kInt8 = false;
   static constexpr int kStagingBytes = 0;
   struct Params {
     const int* tokens_c;   // [rows] compact sampled-token ids
@@ -75,7 +77,7 @@ struct RowStats {
         const float2 t2 = __ffma2_rn(z2, l2, nm2);
         const float2 e2 = make_float2(ex2_approx(t2.x), ex2_approx(t2.y));
         cs2 = __fadd2_rn(cs2, e2);
-        ca2 = __ffma2_rn(e2, z2, ca2);
+        ca2 = SUM ? __fadd2_rn(ca2, z2) : __ffma2_rn(e2, z2, ca2);
       }
       cs = cs2.x + cs2.y;
       ca = ca2.x + ca2.y;
@@ -84,11 +86,11 @@ struct RowStats {
       for (int i = 0; i < 32; ++i) {
         const float e = i < nvalid ? ex2_approx(fmaf(v[i], kLog2e, -mL)) : 0.f;
         cs += e;
-        ca = fmaf(e, v[i], ca);
+        ca = SUM ? (i < nvalid ? ca + v[i] : ca) : fmaf(e, v[i], ca);
       }
     }
     st.s = fmaf(st.s, scale, cs);
-    st.a = fmaf(st.a, scale, ca);
+    st.a = SUM ? st.a + ca : fmaf(st.a, scale, ca);
     st.m = newm;
     const unsigned rel = (unsigned)(st.y - col0);
     if (rel < 32u && (int)rel < nvalid) {
@@ -108,7 +110,7 @@ struct RowStats {
     // a half that saw no column inside the vocabulary has m = -inf and sums of 0
     const float a = st.m == m ? 1.f : ex2_approx((st.m - m) * kLog2e), b = x[0] == m ? 1.f : ex2_approx((x[0] - m) * kLog2e);
     st.s = fmaf(st.s, a, x[1] * b);
-    st.a = fmaf(st.a, a, x[2] * b);
+    st.a = SUM ? st.a + x[2] : fmaf(st.a, a, x[2] * b);
     st.zy += x[3];
     st.m = m;
   }
@@ -119,12 +121,14 @@ struct RowStats {
   }
 };
 
+using RowStats = RowStatsOf<false>;
+
 // With four epilogue warps (one per scheduler) their latencies are exposed and a tile's epilogue takes 3.8 us; with
 // eight it takes 2.7, but they slow the MMA issuer down.  So eight where K is short: 8192 rows x 151936 words, score pass
 // 908 / 1072 / 1377 / 1608 / 3072 us with four, 752 / 949 / 1250 / 1668 / 3718 with eight at d = 256 / 512 / 768 / 1024 / 2048.
 constexpr int kEightWarpsMaxK = 896;
-template <int W>
-struct EpiStats : RowStats {
+template <int W, bool SUM = false>
+struct EpiStats : RowStatsOf<SUM> {
   static constexpr int kWarps = W;
 };
 
@@ -168,15 +172,17 @@ __device__ __forceinline__ void stage_half_box(const uint32_t (&w)[16], int c, u
 // {columns, rows, planes} with boxes of 32 x 32, 64-byte swizzled.  6912 rows x 151936 words: 1.97 / 2.17 / 3.34 / 5.63 ms at
 // d = 896 / 1024 / 2048 / 3584 (eight epilogue warps 1.94 / 2.17 / 3.52 / 5.98; stores straight from registers 1.96 / - / 3.48 / 5.75;
 // the statistics alone 1.36 / 1.65 / 2.85 / 5.16).
-struct EpiSweep {
+template <bool SUM>
+struct EpiSweepOf {
+  using Stats = RowStatsOf<SUM>;
   static constexpr bool kParts = false;
   static constexpr int kSideWarps = 0;
-  static constexpr bool kFeeds = false, kAhead = false;
+  static constexpr bool kFeeds = false, kAhead = false, kInt8 = false;
   static constexpr int kWarps = 4;
   static constexpr int kStagingBytes = kEpiStaging;
-  using Params = RowStats::Params;
+  using Params = typename Stats::Params;
   struct State {
-    RowStats::State s;
+    typename Stats::State s;
     uint32_t n_issued;
     int grow;   // compact row
   };
@@ -201,7 +207,7 @@ struct EpiSweep {
                                                const CUtensorMap* map, uint32_t staging) {
     // a CTA pair may own a 128-row tile that lies wholly past the slab's rows: nothing to write
     if (m_tile * BM >= ((m_rows + BM - 1) / BM) * BM) return;
-    RowStats::chunk(p, st.s, 0, n_tile, c, 0, 0, v, map, staging);
+    Stats::chunk(p, st.s, 0, n_tile, c, 0, 0, v, map, staging);
     const int lane = threadIdx.x & 31;
     constexpr int kBufs = kStagingBytes / kWarps / kBoxBytes;
     const uint32_t buf = staging + (st.n_issued % kBufs) * kBoxBytes;   // 2 KB of upper halves, 2 KB of lower ones
@@ -233,14 +239,15 @@ struct EpiSweep {
     }
     st.n_issued++;
   }
-  static constexpr int kMerge = RowStats::kMerge;
-  __device__ static __forceinline__ void pack(const State& st, float (&x)[kMerge]) { RowStats::pack(st.s, x); }
-  __device__ static __forceinline__ void merge(State& st, const float (&x)[kMerge]) { RowStats::merge(st.s, x); }
+  static constexpr int kMerge = Stats::kMerge;
+  __device__ static __forceinline__ void pack(const State& st, float (&x)[kMerge]) { Stats::pack(st.s, x); }
+  __device__ static __forceinline__ void merge(State& st, const float (&x)[kMerge]) { Stats::merge(st.s, x); }
   __device__ static __forceinline__ void end_unit(const Params& p, State& st, int, int nr, int, int) {
     if (st.grow >= 0)
       p.partials[(size_t)nr * p.part_stride + st.grow] = make_float4(st.s.m, st.s.s, st.s.a, st.s.zy);
   }
 };
+using EpiSweep = EpiSweepOf<false>;
 
 // ---------------------------------------------------------------------------------------------
 // Gradient with respect to the logits for one slab of rows x vocabulary columns, rounded to
@@ -260,12 +267,14 @@ struct GradParams {
   const float* ce;
   int V;
   int vocab_base;  // global column of the slab's column 0
+  float uniform;   // cross entropy: e / ((1 - e) V) of labels smoothed by e
 };
-template <int W>
+// CE: the gradient of the cross entropy, g_tj = cp_t p_tj - ct_t (1[j = y_t] + uniform), ct_t = w_t (1 - e) in place of ce_t.
+template <int W, bool CE = false>
 struct EpiGrad {
   static constexpr bool kParts = false;
   static constexpr int kSideWarps = 0;
-  static constexpr bool kFeeds = false, kAhead = false;
+  static constexpr bool kFeeds = false, kAhead = false, kInt8 = false;
   static constexpr int kWarps = W;
   static constexpr int kMerge = 0;
   static constexpr int kStagingBytes = kEpiStaging;
@@ -282,7 +291,7 @@ struct EpiGrad {
     st.valid = rl < m_rows;
     const int gr = slab_off + rl;   // compact row of this slab row
     st.lse = st.valid ? p.lse[gr] : 0.f;
-    st.ent = st.valid ? p.ent[gr] : 0.f;
+    st.ent = st.valid && !CE ? p.ent[gr] : 0.f;
     st.cp = st.valid ? p.cp[gr] : 0.f;
     st.ce = st.valid ? p.ce[gr] : 0.f;
     st.y = st.valid ? p.tokens_c[gr] : -1;
@@ -305,7 +314,17 @@ struct EpiGrad {
 #pragma unroll
       for (int i = 0; i < 32; ++i) g[i] = 0.f;
     } else {
-      if (st.ce == 0.f) {
+      if (CE) {
+        const float2 l2 = make_float2(kLog2e, kLog2e), nl2 = make_float2(-st.lse * kLog2e, -st.lse * kLog2e);
+        const float2 cp2 = make_float2(st.cp, st.cp), u2 = make_float2(-st.ce * p.uniform, -st.ce * p.uniform);
+#pragma unroll
+        for (int i = 0; i < 32; i += 2) {
+          const float2 t2 = __ffma2_rn(make_float2(v[i], v[i + 1]), l2, nl2);
+          const float2 g2 = __ffma2_rn(make_float2(ex2_approx(t2.x), ex2_approx(t2.y)), cp2, u2);
+          g[i] = g2.x;
+          g[i + 1] = g2.y;
+        }
+      } else if (st.ce == 0.f) {
         // packed fp32 pairs: p = 2^(z*log2e - lse*log2e), g = cp * p
         const float2 l2 = make_float2(kLog2e, kLog2e), nl2 = make_float2(-st.lse * kLog2e, -st.lse * kLog2e);
         const float2 cp2 = make_float2(st.cp, st.cp);
@@ -337,7 +356,7 @@ struct EpiGrad {
       const unsigned rel = (unsigned)(st.y - col_g);
       if (rel < 32u) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) g[i] = (rel == (unsigned)i) ? g[i] - st.cp : g[i];
+        for (int i = 0; i < 32; ++i) g[i] = (rel == (unsigned)i) ? g[i] - (CE ? st.ce : st.cp) : g[i];
       }
       if (nvalid < 32) {
 #pragma unroll
@@ -378,11 +397,12 @@ struct AccParams {
 // DRAM one box at a time.  dW of 151936 words, d = 2048, four warps / eight: stores 282 / 264 us at 100 rows, 380 / 340 at 300, 468 / 430 at
 // 512, and slower from 1000 rows on; adds 542 / 425, 587 / 446, 602 / 524 (the four without prefetches; with them 413 / 494 / 544; a
 // plain kernel that adds in this order takes 400).
-template <int W>
+// HALF: stored as bf16 instead, through a map of 64-column boxes (never added to, tiles not cut).
+template <int W, bool HALF = false>
 struct EpiAccW {
-  static constexpr bool kParts = true;
+  static constexpr bool kParts = !HALF;
   static constexpr int kSideWarps = 0;
-  static constexpr bool kFeeds = false, kAhead = W == 8;
+  static constexpr bool kFeeds = false, kAhead = W == 8 && !HALF, kInt8 = false;
   static constexpr int kWarps = W;
   static constexpr int kMerge = 0;
   static constexpr int kStagingBytes = kEpiStaging;
@@ -409,6 +429,16 @@ struct EpiAccW {
     const int row0 = m_tile * BM + (row_in_tile - lane);   // first row of this warp's 32
     const int col0 = n_tile * BN + c * 32;
     if (row0 >= m_rows || col0 >= p.n_cols) return;        // warp-uniform
+    if constexpr (HALF) {
+      uint32_t w[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+        w[i] = *reinterpret_cast<const uint32_t*>(&b);
+      }
+      stage_half_box<kStagingBytes / kWarps / kBoxBytes>(w, c, staging, st.n_issued, tmC, col0, p.row_base + row0);
+      return;
+    }
     const bool part = p.tile_cols > 0 && st.k_slice > 0;
     constexpr int kBufs = kStagingBytes / kWarps / kBoxBytes;
     const uint32_t buf = staging + (st.n_issued % kBufs) * kBoxBytes;

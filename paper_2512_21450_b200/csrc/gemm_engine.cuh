@@ -1,4 +1,4 @@
-// Persistent, warp-specialised bf16 GEMM main loop for sm_100a with pluggable epilogues.  One
+// Persistent, warp-specialised GEMM main loop (bf16; 8-bit integers where the epilogue says so) for sm_100a with pluggable epilogues.  One
 // kernel template serves every tensor-core pass of the library; a tile mode picks how the two
 // 256-column fp32 accumulators of tensor memory are used.
 //
@@ -474,6 +474,7 @@ struct UnitWalk {
 //     static constexpr bool kAhead;                            // State has next_row and next_col: this warp's first row and column of the next tile
 //     static constexpr int kSideWarps; static constexpr bool kFeeds; };   // if kSideWarps > 0:
 //     static void side(const Params&, const GemmExtents&, int cg, int n_workers, int warp);
+//     static constexpr bool kInt8;                             // 8-bit integer operands (K-major): chunks are the bits of 32-bit integers
 //   if kFeeds:
 //     static bool feeds(const Params&, const GemmExtents&, int n_workers);   // or A is complete when the launch starts
 //     static const unsigned* feed_flag(const Params&, int m_tile, int chunk);
@@ -488,6 +489,9 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
             const typename Epi::Params ep, DevStatus* status) {
   static_assert(MODE != kTileWide || CG == 2, "wide tiles run on CTA pairs");
   static_assert(MODE != kTileDual || (A_MN == 0 && B_MN == 0), "the two-product mode takes K-major operands");
+  static_assert(!Epi::kInt8 || (A_MN == 0 && B_MN == 0 && MODE == kTileSquare), "8-bit operands are K-major, tiles square");
+  // elements of a k-block, which has 128 bytes; extents (GemmShape) count k-blocks of BK whatever the type is
+  constexpr int kBlockK = Epi::kInt8 ? 2 * BK : BK;
   using Cfg = StageCfg<CG, MODE, Epi::kStagingBytes>;
   constexpr int kStages = Cfg::kStages;
   constexpr int kProducts = MODE == kTileDual ? 2 : 1;
@@ -598,8 +602,8 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
               for (int j = 0; j < Cfg::kKSub; ++j) {
                 const uint32_t a_dst = tiles_base + stage * Cfg::kStageBytes + j * Cfg::kSliceBytes;
                 const uint32_t b_dst = a_dst + kAStageBytes;
-                const int a_k = (prod ? 0 : sh.a_k_off) + (kb + j) * BK;
-                const int b_k = (prod ? 0 : sh.b_k_off + (sh.b_k_slab ? ex.slab_off : 0)) + (kb + j) * BK;
+                const int a_k = (prod ? 0 : sh.a_k_off) + (kb + j) * kBlockK;
+                const int b_k = (prod ? 0 : sh.b_k_off + (sh.b_k_slab ? ex.slab_off : 0)) + (kb + j) * kBlockK;
                 if (CG == 1) {
                   if (A_MN) tma_load_3d(a_dst, ta, full, 0, a_k, a_row / 64);
                   else      tma_load_2d(a_dst, ta, full, a_k, a_row);
@@ -637,7 +641,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
   } else if (warp == 1) {
     // ------------------------------------------------------------- MMA issuer (even CTA of a pair)
     if (lane == 0 && rank == 0) {
-      constexpr uint32_t idesc = make_idesc_bf16(BM * CG, BN, A_MN, B_MN);
+      constexpr uint32_t idesc = Epi::kInt8 ? make_idesc_s8(BM * CG, BN) : make_idesc_bf16(BM * CG, BN, A_MN, B_MN);
       // K-major: 8-row groups 1024 B apart, 32 bytes per 16-element k step.
       // MN-major: 64-row panels 8192 B apart, 8-k-line groups 1024 B apart, 2048 B per k step.
       constexpr uint64_t a_hi = A_MN ? make_smem_desc_hi(8192, 1024) : make_smem_desc_hi(16, 1024);
@@ -699,10 +703,12 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
                   for (int k = 0; k < BK / 16; ++k) {
                     const uint32_t acc = (kb > lo || j > 0 || k > 0) ? 1u : 0u;
 #pragma unroll
-                    for (int s = 0; s < Cfg::kBBoxes; ++s)
-                      umma_bf16_words<CG>(d_tmem + s * BN, a_lo + (j * Cfg::kSliceBytes + k * a_kstep) / 16, a_hi32,
-                                          b_lo + (j * Cfg::kSliceBytes + s * Cfg::kBBytes + k * b_kstep) / 16, b_hi32,
-                                          idesc, acc);
+                    for (int s = 0; s < Cfg::kBBoxes; ++s) {
+                      const uint32_t a_w = a_lo + (j * Cfg::kSliceBytes + k * a_kstep) / 16;
+                      const uint32_t b_w = b_lo + (j * Cfg::kSliceBytes + s * Cfg::kBBytes + k * b_kstep) / 16;
+                      if constexpr (Epi::kInt8) umma_i8_words<CG>(d_tmem + s * BN, a_w, a_hi32, b_w, b_hi32, idesc, acc);
+                      else umma_bf16_words<CG>(d_tmem + s * BN, a_w, a_hi32, b_w, b_hi32, idesc, acc);
+                    }
                   }
                 }
                 if (CG == 2) umma_commit_pair_mcast(smem_u32(&bar_empty[stage]), 3);

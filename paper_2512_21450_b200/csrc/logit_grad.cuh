@@ -4,6 +4,8 @@
 //   g_tj = cp_t (p_tj - 1[j = y_t]) + cb_t p_tj (log p_tj - log q_tj - KL_t) + ce_t p_tj (log p_tj + Ent_t),
 // written in place of the policy logits' upper halves; rows past the slab's valid rows (up to a multiple of 128) and
 // columns past V become zero.  4 bytes in (8 with the KL) and 2 out per entry, nothing read twice: bound by memory.
+// With the cross entropy that of EpiGrad<., true>:
+//   g_tj = cp_t p_tj - ct_t (1[j = y_t] + uniform).
 // The work is done by extra warps of the dH kernel (EpiAccFed), which read and write DRAM while the tensor cores
 // multiply what they have finished, or by a kernel of its own (logit_grad_kernel) where dH does not come next, where that does
 // not pay (feed_pays) and with the full KL.
@@ -13,6 +15,8 @@
 #include "kl_epilogues.cuh"
 
 namespace rlh {
+
+enum GradKind { kGradPolicy = 0, kGradKL = 1, kGradCE = 2 };
 
 struct LogitGradParams {
   uint16_t* slab;          // [slab rows][ld] upper halves of the logits, then the gradient
@@ -24,7 +28,8 @@ struct LogitGradParams {
   const float* lse;
   const float* ent;
   const float* cp;
-  const float* ce;
+  const float* ce;         // kGradCE: ct
+  float uniform;
   // full-distribution KL: the reference's logits
   const float* zr;
   const float* lse_ref;
@@ -117,12 +122,12 @@ __host__ __device__ inline void feed_pair(const GemmExtents& ex, const FeedOrder
 // What a row brings to its entries: log-sum-exp; cp, ce and the terms that do not depend on the column; with the KL the
 // reference's log-sum-exp and cb.  valid: not a row of padding.
 struct GradRow {
-  float lse, cp, ce, rest, lse_ref, cb;
+  float lse, cp, ce, rest, lse_ref, cb;   // kGradCE: ce = ct, rest = ct * uniform
   int y;
   bool valid;
 };
 // Eight entries from column c on: halves of the logits (and the reference's logits) to the gradient.
-template <bool KL>
+template <int KIND>
 __device__ __forceinline__ uint4 grad_words(const GradRow& r, const uint4& h, const uint4& l, const float (&zr)[8], int c, int V) {
   const uint32_t hw[4] = {h.x, h.y, h.z, h.w}, lw[4] = {l.x, l.y, l.z, l.w};
   const float k_lp = r.cb + r.ce;   // coefficient of log p_j
@@ -130,9 +135,11 @@ __device__ __forceinline__ uint4 grad_words(const GradRow& r, const uint4& h, co
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     const float z = __uint_as_float(__byte_perm(lw[j / 2], hw[j / 2], j & 1 ? 0x7632 : 0x5410));
-    if constexpr (KL) {
+    if constexpr (KIND == kGradKL) {
       const float lp = z - r.lse;
       g[j] = ex2_approx(lp * kLog2e) * (fmaf(k_lp, lp, r.rest) - r.cb * (zr[j] - r.lse_ref));
+    } else if constexpr (KIND == kGradCE) {
+      g[j] = fmaf(ex2_approx(fmaf(z, kLog2e, -r.lse * kLog2e)), r.cp, -r.rest);
     } else {
       const float e = ex2_approx(fmaf(z, kLog2e, -r.lse * kLog2e));
       g[j] = r.ce == 0.f ? e * r.cp : e * fmaf(r.ce, z - r.lse, r.rest);
@@ -141,7 +148,7 @@ __device__ __forceinline__ uint4 grad_words(const GradRow& r, const uint4& h, co
   const unsigned rel = (unsigned)(r.y - c);
   if (rel < 8u) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) g[j] = rel == (unsigned)j ? g[j] - r.cp : g[j];
+    for (int j = 0; j < 8; ++j) g[j] = rel == (unsigned)j ? g[j] - (KIND == kGradCE ? r.ce : r.cp) : g[j];
   }
   if (!r.valid || c + 8 > V) {
 #pragma unroll
@@ -156,13 +163,15 @@ __device__ __forceinline__ uint4 grad_words(const GradRow& r, const uint4& h, co
   return make_uint4(o[0], o[1], o[2], o[3]);
 }
 // Row i of the compact arrays.
-template <bool KL>
+template <int KIND>
 __device__ __forceinline__ GradRow grad_row(const LogitGradParams& p, int i) {
   GradRow r = {p.lse[i], p.cp[i], p.ce[i], 0.f, 0.f, 0.f, p.tokens_c[i], true};
-  if (KL) {
+  if (KIND == kGradKL) {
     r.lse_ref = p.lse_ref[i];
     r.cb = p.cb[i];
     r.rest = r.cp + r.ce * p.ent[i] - r.cb * p.kl[i];
+  } else if (KIND == kGradCE) {
+    r.rest = r.ce * p.uniform;
   } else {
     r.rest = fmaf(r.ce, p.ent[i], r.cp);
   }
@@ -173,13 +182,14 @@ __device__ __forceinline__ GradRow grad_row(const LogitGradParams& p, int i) {
 // first is used.  151936 columns: 17 / 45 / 146 / 556 / 986 us at 64 / 276 / 1000 / 4000 / 6912 rows, 5.5 TB/s at 276 and 6.3-6.6
 // from 600 on (two pairs in flight 17 / 49 / 150 / 590 / 1089, eight 17 / 49 / 148 / 565 / 1012).  With the KL, four words per output:
 // 68 / 232 / 462 us at 276 / 1000 / 2000 rows (one 256-column step: 72 / 247 / 481).
-template <bool KL>
-constexpr int kGradVecs = KL ? 2 : 4;
+template <int KIND>
+constexpr int kGradVecs = KIND == kGradKL ? 2 : 4;
 // Params: FeedParams where the dH pass may do it.
-template <bool KL, class Params>
+template <int KIND, class Params>
 __global__ void __launch_bounds__(256) logit_grad_kernel(const Params p, const DevStatus* st) {
   chain_begin();
-  constexpr int kVecs = kGradVecs<KL>;
+  constexpr int kVecs = kGradVecs<KIND>;
+  constexpr bool KL = KIND == kGradKL;
   if constexpr (std::is_same<Params, FeedParams>::value) {
     if (feed_pays(gemm_extents(p.dh, st->n_valid, p.cg, p.workers), p.workers)) return;
   }
@@ -215,19 +225,20 @@ __global__ void __launch_bounds__(256) logit_grad_kernel(const Params p, const D
           z1[k] = __ldcs(ref + k * 64 + 1);
         }
       }
-    const GradRow row = grad_row<KL>(p, off + r);
+    const GradRow row = grad_row<KIND>(p, off + r);
 #pragma unroll
     for (int k = 0; k < kVecs; ++k) {
       if (c0 + k * 256 >= p.ld) break;
       const int q = KL ? k : 0;
       const float zr[8] = {z0[q].x, z0[q].y, z0[q].z, z0[q].w, z1[q].x, z1[q].y, z1[q].z, z1[q].w};
-      base[k * 32] = grad_words<KL>(row, h[k], l[k], zr, c0 + k * 256 + lane * 8, p.V);
+      base[k * 32] = grad_words<KIND>(row, h[k], l[k], zr, c0 + k * 256 + lane * 8, p.V);
     }
   }
 }
 
 // By warps of a tensor-core kernel: the jobs of one of them, as long as there are any.  The words of the next two rows are in
 // flight while these are worked on, across jobs.  (Not with the KL: 8 bytes in per entry were too much beside the products, steps level.)
+template <int KIND>   // not kGradKL
 struct LogitGradWarp {
   static constexpr int kStepRows = 2;
   static constexpr int kSteps = kFeedRows / kStepRows;
@@ -264,7 +275,7 @@ struct LogitGradWarp {
       for (int k = 0; k < kVecs; ++k) {
         if (j.c0 + k * 256 >= p.ld) break;
         const int c = j.c0 + k * 256 + lane * 8;
-        *reinterpret_cast<uint4*>(p.slab + (size_t)(j.r0 + rj) * p.ld + c) = grad_words<false>(row, w.h[i][k], w.l[i][k], {}, c, p.V);
+        *reinterpret_cast<uint4*>(p.slab + (size_t)(j.r0 + rj) * p.ld + c) = grad_words<KIND>(row, w.h[i][k], w.l[i][k], {}, c, p.V);
       }
     }
   }
@@ -283,7 +294,7 @@ struct LogitGradWarp {
     const int r = j.r0 + (lane & (kFeedRows - 1));
     j.row = {};
     j.row.y = -1;
-    if (r < rows) j.row = grad_row<false>(p, off + r);
+    if (r < rows) j.row = grad_row<KIND>(p, off + r);
   }
   __device__ static __forceinline__ void run(const FeedParams& p, const GemmExtents& ex, const FeedOrder& o, int off, int rows) {
     const int lane = threadIdx.x & 31;
@@ -319,14 +330,15 @@ struct LogitGradWarp {
 
 // dH of one slab while its operand G is still being formed: kSideWarps warps of every CTA do the jobs of LogitGradWarp, the
 // producer waits for the chunks it is about to load.
-struct EpiAccFed : EpiAcc {
+template <int KIND>
+struct EpiAccFedOf : EpiAcc {
   static constexpr int kSideWarps = 9;   // with the one that watches, sixteen warps in all: 128 registers a thread
   static constexpr bool kFeeds = true;
   struct Params : AccParams {
     FeedParams grad;
   };
   __device__ static __forceinline__ void side(const Params& p, const GemmExtents& ex, int cg, int n_workers, int) {
-    LogitGradWarp::run(p.grad, ex, feed_order(ex, ex.m_rows, p.grad.ld, cg, n_workers), ex.slab_off, ex.m_rows);
+    LogitGradWarp<KIND>::run(p.grad, ex, feed_order(ex, ex.m_rows, p.grad.ld, cg, n_workers), ex.slab_off, ex.m_rows);
   }
   __device__ static __forceinline__ bool feeds(const Params& p, const GemmExtents& ex, int n_workers) { return feed_pays(ex, n_workers); }
   // Counter of column chunk `chunk` of 128-row tile m
@@ -334,5 +346,6 @@ struct EpiAccFed : EpiAcc {
     return p.grad.ready + m * ((p.grad.ld + kFeedCols - 1) / kFeedCols) + chunk;
   }
 };
+using EpiAccFed = EpiAccFedOf<kGradPolicy>;
 
 }  // namespace rlh

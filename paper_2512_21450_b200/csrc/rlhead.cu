@@ -4,6 +4,8 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 
+#include <cmath>
+#include <cstddef>
 #include <cstdio>
 #include <cstring>
 #include <mutex>
@@ -305,6 +307,11 @@ size_t ws_bytes(const rl_ctx* c, int64_t T, int64_t d, int64_t V) {
   return twice > L.total ? twice : L.total;
 }
 
+// Of a cross entropy; round_dW: dW is added up in fp32 behind everything else.
+inline size_t ce_ws_bytes(const WsLayout& L, int64_t d, int64_t V, bool round_dW) {
+  return round_dW ? align_up(L.total, 1024) + (size_t)V * d * 4 : L.total;
+}
+
 // K-major operand: global tensor [rows, k] with k contiguous, row stride ld elements.
 bool map_kmajor(rl_ctx* c, CUtensorMap* m, const void* base, uint64_t rows, uint64_t k, uint64_t ld,
                 uint32_t box_rows) {
@@ -313,6 +320,16 @@ bool map_kmajor(rl_ctx* c, CUtensorMap* m, const void* base, uint64_t rows, uint
   cuuint32_t box[2] = {64, box_rows};
   cuuint32_t es[2] = {1, 1};
   return c->encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, es,
+                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// The same of 8-bit integers; k and ld in elements, ld a multiple of 16.
+bool map_kmajor_i8(rl_ctx* c, CUtensorMap* m, const void* base, uint64_t rows, uint64_t k, uint64_t ld, uint32_t box_rows) {
+  cuuint64_t dims[2] = {k, rows};
+  cuuint64_t strides[1] = {ld};
+  cuuint32_t box[2] = {128, box_rows};
+  cuuint32_t es[2] = {1, 1};
+  return c->encode(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, es,
                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -388,6 +405,24 @@ cudaError_t set_smem_attr_dual() {
   return e != cudaSuccess ? e : set_smem_attr_one<Epi, 0, 0, 2, kTileDual>();
 }
 
+cudaError_t set_smem_attr_int8() {
+  cudaError_t e = set_smem_attr<EpiStatsI8<4>, 0, 0>();
+  auto also = [&](cudaError_t x) { if (e == cudaSuccess) e = x; };
+  also(set_smem_attr<EpiStatsI8<8>, 0, 0>());
+  also(set_smem_attr<EpiScale<kOutBf16, true, 4>, 0, 0>());
+  also(set_smem_attr<EpiScale<kOutF32, true, 4>, 0, 0>());
+  also(set_smem_attr<EpiScale<kOutF16, true, 4>, 0, 0>());
+  also(set_smem_attr<EpiScale<kOutBf16, false, 4>, 0, 0>());
+  also(set_smem_attr<EpiScale<kOutF32, false, 4>, 0, 0>());
+  also(set_smem_attr<EpiScale<kOutF16, false, 4>, 0, 0>());
+  auto few = [&](auto kernel) { also(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewSmem)); };
+  few(int8_few_kernel<1, 8>);
+  few(int8_few_kernel<2, 8>);
+  few(int8_few_kernel<4, 4>);
+  few(int8_few_kernel<8, 4>);
+  return e;
+}
+
 // Rows of B that one CTA stages per k-slice (box height of a K-major B map) and the number of
 // 64-wide panels of an MN-major B map, for the context's CTA grouping.
 inline uint32_t b_box_rows(int cg) { return BN / cg; }
@@ -397,6 +432,18 @@ inline uint32_t b_box_panels(const rl_ctx* c) { return BN / 64 / c->cta_group; }
 // CTAs per row tile of the passes that form logits: a pair would spend half its tensor work on padding when at most 128
 // rows exist, and with so few rows the pass is a stream of W.
 inline int fwd_cta_group(const rl_ctx* c, const WsLayout& L) { return L.Tpad <= BM ? 1 : c->cta_group; }
+
+// The context's device is the current one for as long as this lives.
+struct OnDevice {
+  int before = -1;
+  explicit OnDevice(const rl_ctx* c) {
+    int now = -1;
+    if (cudaGetDevice(&now) == cudaSuccess && now != c->device && cudaSetDevice(c->device) == cudaSuccess) before = now;
+  }
+  ~OnDevice() {
+    if (before >= 0) cudaSetDevice(before);
+  }
+};
 
 // Optional timing of a group of launches: event pair on the context's stream, tagged with a kind.
 int prof_begin(rl_ctx* c, int kind) {
@@ -416,11 +463,12 @@ void prof_end(rl_ctx* c, int i, int kind) {
 
 // One kernel launch on the context's stream that may be scheduled while the launch before it still runs (chain_begin()).
 template <class... P, class... A>
-void launch(rl_ctx* c, void (*kernel)(P...), int grid, int block, A&&... args) {
+void launch_smem(rl_ctx* c, void (*kernel)(P...), int grid, int block, size_t smem, A&&... args) {
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof(cfg));
   cfg.gridDim = dim3(grid);
   cfg.blockDim = dim3(block);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = c->stream;
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -428,6 +476,10 @@ void launch(rl_ctx* c, void (*kernel)(P...), int grid, int block, A&&... args) {
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
   cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
+template <class... P, class... A>
+void launch(rl_ctx* c, void (*kernel)(P...), int grid, int block, A&&... args) {
+  launch_smem(c, kernel, grid, block, 0, static_cast<A&&>(args)...);
 }
 
 // One launch of the tensor-core engine in tile mode MODE on the context's persistent grid (CTA pairs
@@ -483,6 +535,27 @@ void launch_dual(rl_ctx* c, int kind, const CUtensorMap& a, const CUtensorMap& b
   launch_tiles<Epi, 0, 0, kTileDual>(c, c->cta_group, kind, a, b, a2, b2, out, sh, k2_len, ep);
 }
 
+inline rl_status cuda_ok() { return cudaGetLastError() == cudaSuccess ? RL_OK : RL_ERR_CUDA; }
+
+// Product of 8-bit rows on the tensor cores; C through the TMA unit where its rows start and end on 16 bytes.
+template <int OUT>
+rl_status int8_tiles(rl_ctx* c, const CUtensorMap& a, const CUtensorMap& b, int cg, const GemmShape& sh, const ScaleParams& p,
+                            int64_t T) {
+  constexpr int kElem = OUT == kOutF32 ? 4 : 2;
+  // (the TMA unit clips a box at a row's end to 16 bytes: with a V that ends inside them, what lies behind would be written too)
+  const bool tma = (reinterpret_cast<uintptr_t>(p.C) & 15) == 0 && p.ldC * kElem % 16 == 0 && (int64_t)p.V * kElem % 16 == 0;
+  if (!tma) {
+    launch_gemm<EpiScale<OUT, false, 4>, 0, 0>(c, cg, 0, a, b, a, a, sh, p);
+    return cuda_ok();
+  }
+  CUtensorMap out;
+  const bool ok = OUT == kOutF32 ? map_out_f32(c, &out, static_cast<float*>(p.C), (uint64_t)T, (uint64_t)p.V, (uint64_t)p.ldC, 1, (uint64_t)T)
+                                 : map_out_bf16(c, &out, p.C, (uint64_t)T, (uint64_t)p.V, (uint64_t)p.ldC);
+  if (!ok) return RL_ERR_CUDA;
+  launch_gemm<EpiScale<OUT, true, 4>, 0, 0>(c, cg, 0, a, b, out, out, sh, p);
+  return cuda_ok();
+}
+
 rl_status check_hw(const void* H, int64_t ldH, const void* W, int64_t ldW, int64_t T, int64_t d, int64_t V) {
   if (T < 0 || d <= 0 || V <= 0) return RL_ERR_INVALID_ARG;
   if (T > 0 && (!H || !W)) return RL_ERR_INVALID_ARG;
@@ -519,9 +592,32 @@ inline int row_group_tiles(const rl_ctx* c, int64_t k) {
 void launch_merge(rl_ctx* c, const LossParams& p, int64_t rows, int ranges, int slabs = 1) {
   const int blocks = merge_blocks(rows, slabs, ranges);
   auto merge = [&](auto plain, auto clearing) { launch(c, p.n_clear > 0 ? clearing : plain, blocks, kLossThreads, p, c->dstatus); };
-  if (merge_by_thread(rows, ranges)) merge(combine_loss_kernel<1, false>, combine_loss_kernel<1, true>);
-  else merge(combine_loss_kernel<kLossThreads / 32, false>, combine_loss_kernel<kLossThreads / 32, true>);
+  constexpr int kTeam = kLossThreads / 32;
+  if (p.V > 0) {   // cross entropy
+    if (merge_by_thread(rows, ranges)) merge(combine_loss_kernel<1, false, true>, combine_loss_kernel<1, true, true>);
+    else merge(combine_loss_kernel<kTeam, false, true>, combine_loss_kernel<kTeam, true, true>);
+  } else if (merge_by_thread(rows, ranges)) merge(combine_loss_kernel<1, false>, combine_loss_kernel<1, true>);
+  else merge(combine_loss_kernel<kTeam, false>, combine_loss_kernel<kTeam, true>);
   c->launches++;
+}
+
+// A call of the cross entropy (cross_entropy_impl): what it has besides the arguments of the loss calls.
+struct CeArgs {
+  float smooth, z_coef;
+  float* lse_out;
+  float* each_out;
+  int dW_bf16;
+  const float* H_scale;   // H in 8 bits
+};
+
+// fp32 -> bf16, eight values per thread and step: dW that was added up over several slabs.
+__global__ void __launch_bounds__(256) round_bf16_kernel(const float4* __restrict__ x, uint4* __restrict__ y, long long n8) {
+  chain_begin();
+  for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n8; i += (long long)gridDim.x * blockDim.x) {
+    const float4 a = __ldcs(x + 2 * i), b = __ldcs(x + 2 * i + 1);
+    __stcs(y + i, make_uint4(two_halves<kOutBf16>(a.x, a.y), two_halves<kOutBf16>(a.z, a.w), two_halves<kOutBf16>(b.x, b.y),
+                             two_halves<kOutBf16>(b.z, b.w)));
+  }
 }
 
 // Compute capability and SM count (cudaGetDeviceProperties takes 2.5 ms, these two queries a microsecond).
@@ -531,8 +627,6 @@ rl_status device_facts(int device, int* major, int* n_sm) {
     return RL_ERR_CUDA;
   return *major == 10 ? RL_OK : RL_ERR_UNSUPPORTED_ARCH;
 }
-
-inline rl_status cuda_ok() { return cudaGetLastError() == cudaSuccess ? RL_OK : RL_ERR_CUDA; }
 
 // Mask scan of T rows in two launches (three for very many), row_pos may be NULL.
 void launch_mask_scan(rl_ctx* c, const uint8_t* mask, int64_t T, int* block_counts, int* row_map, int* row_pos) {
@@ -553,7 +647,15 @@ struct FwdPlan {
   int64_t vocab_off = 0;     // first vocabulary id of W's rows (vocabulary-parallel head)
   int64_t V_total = 0;       // size of the whole vocabulary for the token-range check (0: V)
   RowOutputs out = {};       // per-row outputs of the call, zeroed where the mask is 0
+  const float* H_scale = nullptr;   // H is stored in 8 bits
+  bool sums = false;         // statistics of the cross entropy (sum of the logits)
+  const float* W_scale = nullptr;   // W is held in 8 bits: the rows are quantised too, and compact behind them lie their scales
 };
+
+// Compact rows in 8 bits, of d <= 2 d bytes: their scales lie behind them.
+inline float* int8_row_scales(const WsLayout& L, char* ws, int64_t d) { return reinterpret_cast<float*>(ws + L.Hc + (size_t)L.Tpad * d); }
+// k extent (GemmShape) of a product of 8-bit integers: the engine counts blocks of 128 bytes in twos
+inline int int8_k(int64_t d) { return (int)((d + 2 * BK - 1) / (2 * BK)) * BK; }
 
 // Mask scan + row compaction + forward statistics.  Leaves per-range partials in the workspace.
 rl_status run_forward(rl_ctx* c, const WsLayout& L, const void* H, int64_t ldH, const void* W, int64_t ldW,
@@ -578,20 +680,25 @@ rl_status run_forward(rl_ctx* c, const WsLayout& L, const void* H, int64_t ldH, 
   pp.row_map = row_map;
   pp.out = plan.out;
   pp.ticket = reinterpret_cast<unsigned*>(reinterpret_cast<char*>(c->dstatus) + kTicketOffset);
+  pp.H_scale = plan.H_scale;
+  pp.scale_c = int8_row_scales(L, ws, d);
+  auto prep = [&](int blocks, auto copy, auto stored, auto to_int8) {
+    launch(c, plan.W_scale ? to_int8 : plan.H_scale ? stored : copy, blocks, 256, pp, c->dstatus);
+  };
   if (T <= kPrepRows) {
     const int pr = prof_begin(c, 5);
     // a row per warp while that takes no more than four blocks per SM; at most 256: kPrepRows / (4 n_sm)
     int rows = (int)align_up((size_t)(T + c->n_sm * 4 - 1) / (c->n_sm * 4), 8);
     if (rows > 256) rows = 256;
     pp.rows_per_block = rows;
-    launch(c, prep_rows_kernel<true>, (int)((T + rows - 1) / rows), 256, pp, c->dstatus);
+    prep((int)((T + rows - 1) / rows), prep_rows_kernel<true, kRowsCopy>, prep_rows_kernel<true, kRowsStored>, prep_rows_kernel<true, kRowsToInt8>);
     prof_end(c, pr, 5);
   } else {
     int* row_pos = reinterpret_cast<int*>(ws + L.row_pos);
     if (plan.scan) launch_mask_scan(c, mask, T, reinterpret_cast<int*>(ws + L.scan_counts), row_map, row_pos);
     pp.row_pos = row_pos;
     const int pr = prof_begin(c, 5);
-    launch(c, prep_rows_kernel<false>, c->n_sm * 8, 256, pp, c->dstatus);
+    prep(c->n_sm * 8, prep_rows_kernel<false, kRowsCopy>, prep_rows_kernel<false, kRowsStored>, prep_rows_kernel<false, kRowsToInt8>);
     prof_end(c, pr, 5);
   }
   c->launches += 1;
@@ -606,14 +713,15 @@ rl_status run_forward(rl_ctx* c, const WsLayout& L, const void* H, int64_t ldH, 
   }
   const int cg = kl ? c->cta_group : fwd_cta_group(c, L);
   CUtensorMap tmA, tmB;
-  if (!map_kmajor(c, &tmA, Hc, (uint64_t)L.Tpad, (uint64_t)d, (uint64_t)d, BM)) return RL_ERR_CUDA;
-  if (!map_kmajor(c, &tmB, W, (uint64_t)V, (uint64_t)d, (uint64_t)ldW, b_box_rows(cg))) return RL_ERR_CUDA;
+  auto map_k = plan.W_scale ? map_kmajor_i8 : map_kmajor;
+  if (!map_k(c, &tmA, Hc, (uint64_t)L.Tpad, (uint64_t)d, (uint64_t)d, BM)) return RL_ERR_CUDA;
+  if (!map_k(c, &tmB, W, (uint64_t)V, (uint64_t)d, (uint64_t)ldW, b_box_rows(cg))) return RL_ERR_CUDA;
   GemmShape sh;
   memset(&sh, 0, sizeof(sh));
   sh.n_valid = &c->dstatus->n_valid;
   sh.m_rows_cap = L.Tpad;
   sh.m_dyn = 1;
-  sh.k_cap = (int)d;
+  sh.k_cap = plan.W_scale ? int8_k(d) : (int)d;
   sh.n_tiles = (int)((V + BN - 1) / BN);
   sh.n_range = 0;  // split chosen on the device from the number of valid rows
   sh.n_split_max = L.part_ranges;
@@ -624,7 +732,20 @@ rl_status run_forward(rl_ctx* c, const WsLayout& L, const void* H, int64_t ldH, 
   ep.partials = reinterpret_cast<float4*>(ws + L.partials);
   ep.part_stride = L.Tpad;
   ep.V = (int)V;
-  if (!kl) {
+  auto stats = [&](auto four, auto eight, const auto& params, int64_t k) {
+    if (k <= kEightWarpsMaxK) launch_gemm<decltype(eight), 0, 0>(c, cg, 0, tmA, tmB, tmA, tmA, sh, params);
+    else                      launch_gemm<decltype(four), 0, 0>(c, cg, 0, tmA, tmB, tmA, tmA, sh, params);   // no output map
+  };
+  if (plan.W_scale) {
+    Int8StatsParams ei;
+    static_cast<RowStats::Params&>(ei) = ep;
+    ei.row_scale = pp.scale_c;
+    ei.col_scale = plan.W_scale;
+    stats(EpiStatsI8<4>(), EpiStatsI8<8>(), ei, int8_k(d));
+  } else if (plan.sums) {
+    RowStatsOf<true>::Params es = {ep.tokens_c, ep.partials, ep.part_stride, ep.V};
+    stats(EpiStats<4, true>(), EpiStats<8, true>(), es, d);
+  } else if (!kl) {
     if (d <= kEightWarpsMaxK) launch_gemm<EpiStats<8>, 0, 0>(c, cg, 0, tmA, tmB, tmA, tmA, sh, ep);
     else                      launch_gemm<EpiStats<4>, 0, 0>(c, cg, 0, tmA, tmB, tmA, tmA, sh, ep);   // no output map
   } else {
@@ -716,7 +837,13 @@ rl_status rl_create(rl_ctx** out, int device) {
             set_smem_attr_dual<EpiStatsKL>() == cudaSuccess && set_smem_attr_dual<EpiGradKL>() == cudaSuccess &&
             set_smem_attr_one<EpiAcc, 0, 1, 2, kTileWide>() == cudaSuccess &&
             set_smem_attr<EpiAccScatter<4>, 1, 1>() == cudaSuccess && set_smem_attr<EpiAccScatter<8>, 1, 1>() == cudaSuccess && set_smem_attr<EpiAccFed, 0, 1>() == cudaSuccess &&
-            set_smem_attr_one<EpiAccFed, 0, 1, 2, kTileWide>() == cudaSuccess;
+            set_smem_attr_one<EpiAccFed, 0, 1, 2, kTileWide>() == cudaSuccess &&
+            set_smem_attr<EpiStats<4, true>, 0, 0>() == cudaSuccess && set_smem_attr<EpiStats<8, true>, 0, 0>() == cudaSuccess &&
+            set_smem_attr<EpiSweepOf<true>, 0, 0>() == cudaSuccess && set_smem_attr<EpiGrad<4, true>, 0, 0>() == cudaSuccess &&
+            set_smem_attr<EpiGrad<8, true>, 0, 0>() == cudaSuccess && set_smem_attr<EpiAccFedOf<kGradCE>, 0, 1>() == cudaSuccess &&
+            set_smem_attr_one<EpiAccFedOf<kGradCE>, 0, 1, 2, kTileWide>() == cudaSuccess &&
+            set_smem_attr<EpiAccW<4, true>, 1, 1>() == cudaSuccess && set_smem_attr<EpiAccScatter<4, true>, 1, 1>() == cudaSuccess &&
+            set_smem_attr<EpiAccScatter<8, true>, 1, 1>() == cudaSuccess && set_smem_attr_int8() == cudaSuccess;
   if (!ok) { cudaFree(c->dstatus); delete c; return RL_ERR_CUDA; }
   {
     // how many CTA pairs can be resident at once (pairs must share a TPC): the persistent grid
@@ -1119,18 +1246,15 @@ rl_status rl_mask_scan(rl_ctx* c, const uint8_t* mask, int64_t T, int32_t* row_m
   return cuda_ok();
 }
 
-rl_status rl_token_logprobs(rl_ctx* c, const void* H, int64_t ldH, const void* W, int64_t ldW, const int32_t* tokens,
-                            const uint8_t* mask, int64_t T, int64_t d, int64_t V, float* logp, float* entropy,
-                            float* lse) {
-  if (!c) return RL_ERR_INVALID_ARG;
-  rl_status s = check_hw(H, ldH, W, ldW, T, d, V);
-  if (s != RL_OK) return s;
-  if (T == 0) return RL_OK;
-  if (!tokens || !logp) return RL_ERR_INVALID_ARG;
+// Body of rl_token_logprobs and (w_scale: W in 8-bit integers) of rl_token_logprobs_int8.
+static rl_status score(rl_ctx* c, const void* H, int64_t ldH, const void* W, int64_t ldW, const float* w_scale, const int32_t* tokens,
+                       const uint8_t* mask, int64_t T, int64_t d, int64_t V, float* logp, float* entropy, float* lse) {
+  rl_status s;
   const WsLayout L = ws_layout(c, T, d, V, false);
   if ((s = check_ws(c, L.G)) != RL_OK) return s;   // the forward arrays
   char* ws = static_cast<char*>(c->ws);
   FwdPlan plan;
+  plan.W_scale = w_scale;
   plan.out.value[0] = logp; plan.out.value[1] = entropy; plan.out.value[2] = lse;
   if ((s = run_forward(c, L, H, ldH, W, ldW, tokens, mask, T, d, V, nullptr, plan)) != RL_OK) return s;
   LossParams p;
@@ -1148,18 +1272,30 @@ rl_status rl_token_logprobs(rl_ctx* c, const void* H, int64_t ldH, const void* W
   return cuda_ok();
 }
 
-// Body of rl_policy_loss_fwd_bwd_ex (shard == NULL) and of rl_policy_loss_shard_bwd.
+rl_status rl_token_logprobs(rl_ctx* c, const void* H, int64_t ldH, const void* W, int64_t ldW, const int32_t* tokens,
+                            const uint8_t* mask, int64_t T, int64_t d, int64_t V, float* logp, float* entropy,
+                            float* lse) {
+  if (!c) return RL_ERR_INVALID_ARG;
+  rl_status s = check_hw(H, ldH, W, ldW, T, d, V);
+  if (s != RL_OK) return s;
+  if (T == 0) return RL_OK;
+  if (!tokens || !logp) return RL_ERR_INVALID_ARG;
+  return score(c, H, ldH, W, ldW, nullptr, tokens, mask, T, d, V, logp, entropy, lse);
+}
+
+// Body of rl_policy_loss_fwd_bwd_ex (shard == NULL), of rl_policy_loss_shard_bwd and of rl_cross_entropy_fwd_bwd (ce != NULL: either
+// gradient may be left out).
 static rl_status loss_fwd_bwd_impl(rl_ctx* c, const void* H, int64_t ldH, const void* W, int64_t ldW,
                                    const int32_t* tokens, const float* old_logp, const float* ref_logp,
                                    const float* adv, const uint8_t* mask, int64_t T, int64_t d, int64_t V,
                                    float eps_low, float eps_high, float beta, float* loss, void* dH, float* dW,
-                                   const rl_loss_opts* opts, const ShardArgs* shard) {
+                                   const rl_loss_opts* opts, const ShardArgs* shard, const CeArgs* ce = nullptr) {
   if (!c) return RL_ERR_INVALID_ARG;
   rl_status s = check_hw(H, ldH, W, ldW, T, d, V);
   if (s != RL_OK) return s;
   if (!(eps_low >= 0.f && eps_low < 1.f) || !(eps_high >= 0.f) || !(beta >= 0.f)) return RL_ERR_INVALID_ARG;
-  if (!loss || !dW || !W) return RL_ERR_INVALID_ARG;
-  if (T > 0 && (!tokens || !old_logp || !adv || !dH)) return RL_ERR_INVALID_ARG;
+  if (!loss || !W || (!dW && !ce)) return RL_ERR_INVALID_ARG;
+  if (T > 0 && (!tokens || (!ce && (!old_logp || !adv || !dH)))) return RL_ERR_INVALID_ARG;
   rl_loss_opts o;
   memset(&o, 0, sizeof(o));
   if (opts) {
@@ -1197,13 +1333,16 @@ static rl_status loss_fwd_bwd_impl(rl_ctx* c, const void* H, int64_t ldH, const 
   WsLayout L = ws_layout(c, T, d, V, 0, o.kl_full ? o.d_ref : 0);
   // the coefficients of a response's rows need rows of other slabs: the logits are formed twice
   if (seq_path && L.n_row_slabs > 1) L = ws_layout(c, T, d, V, 0, 0, true);
-  if ((s = check_ws(c, L.total)) != RL_OK) return s;
+  const bool backward = dH || dW;
+  // dW in bf16 is written where it is formed, unless it is added up over several slabs: then in fp32 behind everything else
+  const bool round_dW = dW && ce && ce->dW_bf16 && L.n_row_slabs > 1, half_dW = ce && ce->dW_bf16 && !round_dW;
+  if ((s = check_ws(c, !backward && T > 0 ? L.G : ce_ws_bytes(L, d, V, round_dW))) != RL_OK) return s;
   char* ws = static_cast<char*>(c->ws);
   cudaStream_t st = c->stream;
 
   if (T == 0) {
     cudaMemsetAsync(loss, 0, 4, st);
-    if (!o.accumulate_dW) cudaMemsetAsync(dW, 0, (size_t)V * d * 4, st);
+    if (dW && !o.accumulate_dW) cudaMemsetAsync(dW, 0, (size_t)V * d * (ce && ce->dW_bf16 ? 2 : 4), st);
     if (o.metrics_out) cudaMemsetAsync(o.metrics_out, 0, 32, st);
     return cuda_ok();
   }
@@ -1212,12 +1351,18 @@ static rl_status loss_fwd_bwd_impl(rl_ctx* c, const void* H, int64_t ldH, const 
   // forms their logits leave them there in fp32, and an elementwise pass turns them into the gradient once the rows'
   // coefficients are known.  Not where the coefficients of a row need rows of another slab, nor where the
   // statistics come from elsewhere: those paths form the logits a second time.
-  const bool sweep = L.keeps_logits && !shard && (L.n_row_slabs == 1 || !seq_path);
+  const bool sweep = backward && L.keeps_logits && !shard && (L.n_row_slabs == 1 || !seq_path);
   FwdPlan plan;
   plan.out.dH = dH;
   plan.out.dH_row_bytes = (long long)d * (o.dH_dtype ? 4 : 2);
   plan.out.value[0] = o.logp_out; plan.out.value[1] = o.entropy_out;
   plan.out.value[2] = o.kl_full ? o.kl_out : nullptr;
+  if (ce) {
+    plan.out.value[1] = ce->lse_out;
+    plan.out.value[2] = ce->each_out;
+    plan.H_scale = ce->H_scale;
+    plan.sums = true;
+  }
   if (sweep) plan.stats = false;
   if (shard) {
     // the statistics of the whole vocabulary are given: only the row compaction is needed
@@ -1252,6 +1397,13 @@ static rl_status loss_fwd_bwd_impl(rl_ctx* c, const void* H, int64_t ldH, const 
   if (seq_path) p.logp_c = reinterpret_cast<float*>(ws + L.logp_c);
   p.logp_out = o.logp_out;
   p.ent_out = o.entropy_out;
+  if (ce) {
+    p.smooth = ce->smooth;
+    p.z_coef = ce->z_coef;
+    p.V = (int)V;
+    p.lse_out = ce->lse_out;
+    p.each_out = ce->each_out;
+  }
   if (shard) {
     p.ext_logp = shard->logp;
     p.ext_ent = shard->entropy;
@@ -1324,6 +1476,8 @@ static rl_status loss_fwd_bwd_impl(rl_ctx* c, const void* H, int64_t ldH, const 
     prof_end(c, pr_loss, 6);
   };
   if (!sweep) merge_and_loss(0);
+  if (!backward) return cuda_ok();
+  float* dW_f32 = round_dW ? reinterpret_cast<float*>(ws + align_up(L.total, 1024)) : dW;
   // ---- backward, one (row slab x vocabulary slab) at a time
   __nv_bfloat16* Hc = reinterpret_cast<__nv_bfloat16*>(ws + L.Hc);
   __nv_bfloat16* G = reinterpret_cast<__nv_bfloat16*>(ws + L.G);
@@ -1346,7 +1500,8 @@ static rl_status loss_fwd_bwd_impl(rl_ctx* c, const void* H, int64_t ldH, const 
             map_mnmajor(c, &tmHc_mn, Hc, (uint64_t)L.Tpad, (uint64_t)d, (uint64_t)d, b_box_panels(c)) &&
             map_out_bf16(c, &tm_G_out, G, (uint64_t)L.Ts, (uint64_t)L.Vs, (uint64_t)L.Vs) &&
             map_out_f32(c, &tm_dH, dH_acc, (uint64_t)L.Ts, (uint64_t)d, (uint64_t)d, (uint64_t)dh_buffers(c), (uint64_t)L.Ts) &&
-            map_out_f32(c, &tm_dW, dW, (uint64_t)V, (uint64_t)d, (uint64_t)d, 1, (uint64_t)V);
+            (!dW || (half_dW ? map_out_bf16(c, &tm_dW, dW, (uint64_t)V, (uint64_t)d, (uint64_t)d)
+                             : map_out_f32(c, &tm_dW, dW_f32, (uint64_t)V, (uint64_t)d, (uint64_t)d, 1, (uint64_t)V)));
   const int dh_tile_rows = BM * c->cta_group, dh_cols = dh_tile_cols(c, d);
   const int dh_workers = c->grid[c->cta_group] / c->cta_group;
   float* dH_slots = reinterpret_cast<float*>(ws + L.dH_slots);
@@ -1369,11 +1524,12 @@ static rl_status loss_fwd_bwd_impl(rl_ctx* c, const void* H, int64_t ldH, const 
   const int n_col_slabs = (int)((V + L.Vs - 1) / L.Vs);
   const int d_tiles = (int)((d + BN - 1) / BN);
   int hook_slab = 0;
-  const bool dH_beside = dH_beside_dW(c, T, d, V - (int64_t)(n_col_slabs - 1) * L.Vs);
+  const bool dH_beside = dH && dW && dH_beside_dW(c, T, d, V - (int64_t)(n_col_slabs - 1) * L.Vs);
+  const float uniform = ce ? ce->smooth / ((1.f - ce->smooth) * (float)V) : 0.f;
   // Slabs are sized for T rows, and how many of them have any is known to the device alone.  Whoever wants to be told as rows of dW
   // are completed has them walked from the last to the first, so that the one that completes them has rows: its dW launches, in
   // pieces and before its dH, are what is told about while they and dH still run.
-  const bool reverse = c->dw_hook && n_row_slabs > 1;
+  const bool reverse = c->dw_hook && dW && n_row_slabs > 1;
   for (int q = 0; q < n_row_slabs; ++q) {
     const int r = reverse ? n_row_slabs - 1 - q : q;
     GemmShape dh_shape;
@@ -1398,8 +1554,8 @@ static rl_status loss_fwd_bwd_impl(rl_ctx* c, const void* H, int64_t ldH, const 
       const int cols = (int)((V - vocab_base) < L.Vs ? (V - vocab_base) : L.Vs);
       // dH may form its operand itself where it comes next and takes its tiles whole or cut; whether it does is decided on the
       // device (feed_pays), and logit_grad_kernel has nothing to do then
-      const bool report = c->dw_hook && q == n_row_slabs - 1;
-      const bool fed = sweep && !report && !o.kl_full && dh_cuts_tiles(c) && (long long)L.Ts * L.Vs >= kFeedEntries;
+      const bool report = c->dw_hook && dW && q == n_row_slabs - 1;
+      const bool fed = sweep && dH && !report && !o.kl_full && dh_cuts_tiles(c) && (long long)L.Ts * L.Vs >= kFeedEntries;
       // how tiles of dH are cut depends only on rows, d tiles and grid: same for every column slab
       dh_shape.n_valid = n_valid;
       dh_shape.m_rows_cap = rows_cap; dh_shape.m_dyn = 1; dh_shape.slab_cap = L.Tc; dh_shape.slab_one = L.Ts; dh_shape.slab_index = r;
@@ -1454,6 +1610,9 @@ static rl_status loss_fwd_bwd_impl(rl_ctx* c, const void* H, int64_t ldH, const 
             ek.lo = z_lo;
             ek.ld = L.Vs;
             launch_gemm<EpiSweepKL, 0, 0>(c, cg_fwd, 0, tmHc_k, tmW_fwd, tm_G_out, tm_G_out, sw, ek);
+          } else if (ce) {
+            EpiSweepOf<true>::Params es = {ep.tokens_c, ep.partials, ep.part_stride, ep.V};
+            launch_gemm<EpiSweepOf<true>, 0, 0>(c, cg_fwd, 0, tmHc_k, tmW_fwd, tm_planes, tm_planes, sw, es);
           } else {
             launch_gemm<EpiSweep, 0, 0>(c, cg_fwd, 0, tmHc_k, tmW_fwd, tm_planes, tm_planes, sw, ep);
           }
@@ -1469,6 +1628,7 @@ static rl_status loss_fwd_bwd_impl(rl_ctx* c, const void* H, int64_t ldH, const 
           lg.slab_cap = L.Tc; lg.slab_one = L.Ts; lg.slab_index = r;
           lg.tokens_c = ep.tokens_c;
           lg.lse = p.lse_c; lg.ent = p.ent_c; lg.cp = p.cp_c; lg.ce = p.ce_c;
+          lg.uniform = uniform;
           lg.zr = zr;
           lg.lse_ref = p.lse_ref_c; lg.kl = p.kl_c; lg.cb = p.cb_c;
           if (fed) {
@@ -1481,16 +1641,20 @@ static rl_status loss_fwd_bwd_impl(rl_ctx* c, const void* H, int64_t ldH, const 
           {
             const int pr_lg = prof_begin(c, 1);
             const long long padded = (long long)align_up(rows_cap, 128);
-            const int unit = 256 * (o.kl_full ? kGradVecs<true> : kGradVecs<false>);
+            const int unit = 256 * (o.kl_full ? kGradVecs<kGradKL> : kGradVecs<kGradPolicy>);
             long long grad_blocks = (padded * ((L.Vs + unit - 1) / unit) + 7) / 8;   // a warp each
             // many waves of blocks; two where dH may do it, 50 us of blocks that find nothing to do otherwise (6912 rows, d = 2048:
             // 11.03 -> 10.98 ms; 2000 and 4096 rows, which it does not do, level)
             const int most = c->n_sm * (fed ? 6 : 64);
             if (grad_blocks > most) grad_blocks = most;
             const LogitGradParams& alone = lg;
-            if (fed)            launch(c, logit_grad_kernel<false, FeedParams>, (int)grad_blocks, 256, lg, c->dstatus);
-            else if (o.kl_full) launch(c, logit_grad_kernel<true, LogitGradParams>, (int)grad_blocks, 256, alone, c->dstatus);
-            else                launch(c, logit_grad_kernel<false, LogitGradParams>, (int)grad_blocks, 256, alone, c->dstatus);
+            auto grad = [&](auto fed_kernel, auto kernel) {
+              if (fed) launch(c, fed_kernel, (int)grad_blocks, 256, lg, c->dstatus);
+              else     launch(c, kernel, (int)grad_blocks, 256, alone, c->dstatus);
+            };
+            if (o.kl_full) launch(c, logit_grad_kernel<kGradKL, LogitGradParams>, (int)grad_blocks, 256, alone, c->dstatus);
+            else if (ce)   grad(logit_grad_kernel<kGradCE, FeedParams>, logit_grad_kernel<kGradCE, LogitGradParams>);
+            else           grad(logit_grad_kernel<kGradPolicy, FeedParams>, logit_grad_kernel<kGradPolicy, LogitGradParams>);
             prof_end(c, pr_lg, 1);
             c->launches++;
           }
@@ -1509,11 +1673,13 @@ static rl_status loss_fwd_bwd_impl(rl_ctx* c, const void* H, int64_t ldH, const 
             GradParams ep;
             ep.tokens_c = reinterpret_cast<const int*>(ws + L.tokens_c);
             ep.lse = p.lse_c; ep.ent = p.ent_c; ep.cp = p.cp_c; ep.ce = p.ce_c;
-            ep.V = (int)V; ep.vocab_base = vocab_base;
-            if (d <= kEightWarpsMaxK)
-              launch_gemm<EpiGrad<8>, 0, 0>(c, c->cta_group, 1, tmHc_k, tmW_k, tm_G_out, tm_G_out, sh, ep);
-            else
-              launch_gemm<EpiGrad<4>, 0, 0>(c, c->cta_group, 1, tmHc_k, tmW_k, tm_G_out, tm_G_out, sh, ep);
+            ep.V = (int)V; ep.vocab_base = vocab_base; ep.uniform = uniform;
+            auto grad = [&](auto four, auto eight) {
+              if (d <= kEightWarpsMaxK) launch_gemm<decltype(eight), 0, 0>(c, c->cta_group, 1, tmHc_k, tmW_k, tm_G_out, tm_G_out, sh, ep);
+              else                      launch_gemm<decltype(four), 0, 0>(c, c->cta_group, 1, tmHc_k, tmW_k, tm_G_out, tm_G_out, sh, ep);
+            };
+            if (ce) grad(EpiGrad<4, true>(), EpiGrad<8, true>());
+            else    grad(EpiGrad<4>(), EpiGrad<8>());
           } else {
             EpiGradKL::Params ep;
             ep.tokens_c = reinterpret_cast<const int*>(ws + L.tokens_c);
@@ -1536,19 +1702,24 @@ static rl_status loss_fwd_bwd_impl(rl_ctx* c, const void* H, int64_t ldH, const 
           if (use_wide(c, d)) launch_wide<Epi, 0, 1>(c, 2, tmG_k, tmW_mn, tm_dH, tm_slots, sh, params);
           else launch_gemm<Epi, 0, 1>(c, c->cta_group, 2, tmG_k, tmW_mn, tm_dH, tm_slots, sh, params);
         };
-        if (fed) {
-          EpiAccFed::Params params = {};
+        auto fed_tiles = [&](auto epi) {
+          typename decltype(epi)::Params params = {};
           static_cast<AccParams&>(params) = ep;
           params.grad = lg;
-          tiles(EpiAccFed(), params);
+          tiles(epi, params);
+        };
+        if (fed && ce) {
+          fed_tiles(EpiAccFedOf<kGradCE>());
+        } else if (fed) {
+          fed_tiles(EpiAccFed());
         } else {
           tiles(EpiAcc(), ep);
         }
       };
       // (3) dW_slab (+)= G^T * H_slab      [vocabulary rows x d], K = valid rows of the slab
-      if (!report) launch_dH();
+      if (dH && !report) launch_dH();
       const int step = report && cols > kSlabColsMax ? kSlabColsMax : cols;
-      for (int c0 = 0; c0 < cols; c0 += step) {
+      for (int c0 = 0; dW && c0 < cols; c0 += step) {
         GemmShape sh;
         memset(&sh, 0, sizeof(sh));
         sh.n_valid = n_valid;
@@ -1574,8 +1745,12 @@ static rl_status loss_fwd_bwd_impl(rl_ctx* c, const void* H, int64_t ldH, const 
           };
           // (a worker with one or two tiles has nothing for more epilogue warps to overlap: the smallest step 52.2 -> 52.9 us)
           const long long tiles = (long long)d_tiles * ((cols + BN - 1) / BN);
-          if (T <= kFewRows && tiles >= 4 * dh_workers) dW_and_dH(EpiAccScatter<8>());
-          else                                          dW_and_dH(EpiAccScatter<4>());
+          const bool eight = T <= kFewRows && tiles >= 4 * dh_workers;
+          if (half_dW)    eight ? dW_and_dH(EpiAccScatter<8, true>()) : dW_and_dH(EpiAccScatter<4, true>());
+          else if (eight) dW_and_dH(EpiAccScatter<8>());
+          else            dW_and_dH(EpiAccScatter<4>());
+        } else if (half_dW) {
+          launch_gemm<EpiAccW<4, true>, 1, 1>(c, c->cta_group, 3, tmG_mn, tmHc_mn, tm_dW, tm_dW, sh, ep);
         } else {
           launch_gemm<EpiAcc, 1, 1>(c, c->cta_group, 3, tmG_mn, tmHc_mn, tm_dW, tm_dW, sh, ep);
         }
@@ -1585,16 +1760,24 @@ static rl_status loss_fwd_bwd_impl(rl_ctx* c, const void* H, int64_t ldH, const 
           c->dw_hook(c->dw_hook_user, hook_slab++, row0, row0 + sh.m_rows_cap);
         }
       }
-      if (report) launch_dH();
+      if (dH && report) launch_dH();
     }
     // dW of the last column slab has written dH in passing, unless it came before dH or is too short for that
-    if (!dH_beside || (c->dw_hook && q == n_row_slabs - 1)) {
+    if (dH && (!dH_beside || (c->dw_hook && q == n_row_slabs - 1))) {
       src.shape = dh_shape;
       const int pr_sc = prof_begin(c, 7);
       launch(c, scatter_dH_kernel, c->n_sm * 8, 256, src, c->dstatus);
       prof_end(c, pr_sc, 7);
       c->launches++;
     }
+  }
+  if (round_dW) {
+    const long long n8 = (long long)V * d / 8, blocks = (n8 + 255) / 256;
+    const int pr_rd = prof_begin(c, 3);
+    launch(c, round_bf16_kernel, (int)(blocks < c->n_sm * 16 ? blocks : c->n_sm * 16), 256, reinterpret_cast<const float4*>(dW_f32),
+           reinterpret_cast<uint4*>(dW), n8);
+    prof_end(c, pr_rd, 3);
+    c->launches++;
   }
   return cuda_ok();
 }
@@ -1606,6 +1789,163 @@ rl_status rl_policy_loss_fwd_bwd_ex(rl_ctx* c, const void* H, int64_t ldH, const
                                     const rl_loss_opts* opts) {
   return loss_fwd_bwd_impl(c, H, ldH, W, ldW, tokens, old_logp, ref_logp, adv, mask, T, d, V, eps_low, eps_high, beta,
                            loss, dH, dW, opts, nullptr);
+}
+
+rl_status rl_workspace_bytes_ce(rl_ctx* c, int64_t T, int64_t d, int64_t V, int dW_dtype, size_t* bytes) {
+  if (!c || !bytes || T < 0 || d <= 0 || V <= 0 || (dW_dtype != RL_BF16 && dW_dtype != RL_FP32)) return RL_ERR_INVALID_ARG;
+  const WsLayout L = ws_layout(c, T, d, V, 0);
+  *bytes = ce_ws_bytes(L, d, V, dW_dtype == RL_BF16 && L.n_row_slabs > 1);
+  return RL_OK;
+}
+
+rl_status rl_cross_entropy_fwd_bwd(rl_ctx* c, const void* H, int64_t ldH, const void* W, int64_t ldW, const int32_t* targets,
+                                   const uint8_t* mask, int64_t T, int64_t d, int64_t V, float* loss, void* dH, void* dW,
+                                   const rl_ce_opts* opts) {
+  if (!c) return RL_ERR_INVALID_ARG;
+  rl_ce_opts o;
+  memset(&o, 0, sizeof(o));
+  o.dW_dtype = RL_FP32;
+  if (opts) {
+    if (opts->struct_size < offsetof(rl_ce_opts, token_weight) || opts->struct_size > sizeof(o)) return RL_ERR_INVALID_ARG;
+    memcpy(&o, opts, opts->struct_size);
+  }
+  // a smoothed label keeps some of its weight; comparisons are false for NaN
+  if (!(o.label_smoothing >= 0.f && o.label_smoothing < 1.f) || !(o.z_coef >= 0.f && std::isfinite(o.z_coef))) return RL_ERR_INVALID_ARG;
+  if ((o.dH_dtype != RL_BF16 && o.dH_dtype != RL_FP32) || (o.dW_dtype != RL_BF16 && o.dW_dtype != RL_FP32)) return RL_ERR_INVALID_ARG;
+  if (dW && o.dW_dtype == RL_BF16 && (o.accumulate_dW || c->dw_hook)) return RL_ERR_INVALID_ARG;
+  if (o.H_scale && T > 0 && (ldH % 16 != 0)) return RL_ERR_ALIGNMENT;
+  const OnDevice on(c);
+  rl_loss_opts lo;
+  memset(&lo, 0, sizeof(lo));
+  lo.struct_size = sizeof(lo);
+  lo.token_weight = o.token_weight;
+  lo.token_count = o.token_count;
+  lo.accumulate_dW = o.accumulate_dW;
+  lo.logp_out = o.logp_out;
+  lo.metrics_out = o.metrics_out;
+  lo.dH_dtype = o.dH_dtype;
+  const CeArgs ce = {o.label_smoothing, o.z_coef, o.lse_out, o.token_loss_out, o.dW_dtype == RL_BF16, o.H_scale};
+  return loss_fwd_bwd_impl(c, H, ldH, W, ldW, targets, nullptr, nullptr, nullptr, mask, T, d, V, 0.f, 0.f, 0.f, loss, dH,
+                           static_cast<float*>(dW), &lo, nullptr, &ce);
+}
+
+rl_status rl_quantize_rows(rl_ctx* c, const void* X, int x_dtype, int64_t ldX, int64_t rows, int64_t d, int8_t* Q, int64_t ldQ,
+                           float* scale) {
+  if (!c || rows < 0 || d <= 0 || x_dtype < RL_BF16 || x_dtype > RL_FP16) return RL_ERR_INVALID_ARG;
+  if (rows == 0) return RL_OK;
+  if (!X || !Q || !scale) return RL_ERR_INVALID_ARG;
+  if (ldX < d || ldQ < d || rows >= (int64_t(1) << 31) || d >= (int64_t(1) << 30)) return RL_ERR_SHAPE;
+  const uintptr_t elem = x_dtype == RL_FP32 ? 4 : 2, at = reinterpret_cast<uintptr_t>(X);
+  if (at % elem || (reinterpret_cast<uintptr_t>(scale) & 3) || (reinterpret_cast<uintptr_t>(Q) & 15) || ldQ % 16) return RL_ERR_ALIGNMENT;
+  const OnDevice on(c);
+  const bool vec = at % 16 == 0 && ldX * elem % 16 == 0;
+  int64_t blocks = (rows + 7) / 8;   // a warp per row
+  if (blocks > (int64_t)c->n_sm * 64) blocks = (int64_t)c->n_sm * 64;
+  const int pr = prof_begin(c, 5);
+  auto rows_of = [&](auto* x, auto by_vec, auto by_one) {
+    launch(c, vec ? by_vec : by_one, (int)blocks, 256, x, ldX, rows, d, Q, ldQ, scale);
+  };
+  if (x_dtype == RL_BF16) rows_of(static_cast<const __nv_bfloat16*>(X), quantize_rows_kernel<__nv_bfloat16, true>, quantize_rows_kernel<__nv_bfloat16, false>);
+  else if (x_dtype == RL_FP16) rows_of(static_cast<const __half*>(X), quantize_rows_kernel<__half, true>, quantize_rows_kernel<__half, false>);
+  else rows_of(static_cast<const float*>(X), quantize_rows_kernel<float, true>, quantize_rows_kernel<float, false>);
+  prof_end(c, pr, 5);
+  c->launches++;
+  return cuda_ok();
+}
+
+// What both products of 8-bit rows ask of their arguments.
+static rl_status check_int8(const void* B, int64_t ldB, const float* b_scale, int64_t T, int64_t d, int64_t V, const void* C, int c_dtype,
+                            int64_t ldC) {
+  if (T < 0 || d <= 0 || V <= 0 || c_dtype < RL_BF16 || c_dtype > RL_FP16) return RL_ERR_INVALID_ARG;
+  if (!B || !b_scale || (T > 0 && !C)) return RL_ERR_INVALID_ARG;
+  // 2^17 - 1 products of -128 with -128 still fit 32 bits
+  if (d >= (1 << 17) || T >= (int64_t(1) << 30) || V >= (int64_t(1) << 30) || ldB < d || ldC < V) return RL_ERR_SHAPE;
+  const uintptr_t elem = c_dtype == RL_FP32 ? 4 : 2;
+  if ((reinterpret_cast<uintptr_t>(B) & 15) || ldB % 16 || (reinterpret_cast<uintptr_t>(b_scale) & 15) || reinterpret_cast<uintptr_t>(C) % elem)
+    return RL_ERR_ALIGNMENT;
+  return RL_OK;
+}
+
+rl_status rl_int8_matmul(rl_ctx* c, const int8_t* A, int64_t ldA, const float* a_scale, const int8_t* B, int64_t ldB, const float* b_scale,
+                         int64_t T, int64_t d, int64_t V, void* C, int c_dtype, int64_t ldC) {
+  if (!c) return RL_ERR_INVALID_ARG;
+  rl_status s = check_int8(B, ldB, b_scale, T, d, V, C, c_dtype, ldC);
+  if (s != RL_OK) return s;
+  if (T == 0) return RL_OK;
+  if (!A || !a_scale) return RL_ERR_INVALID_ARG;
+  if (ldA < d) return RL_ERR_SHAPE;
+  if ((reinterpret_cast<uintptr_t>(A) & 15) || ldA % 16 || (reinterpret_cast<uintptr_t>(a_scale) & 3)) return RL_ERR_ALIGNMENT;
+  const OnDevice on(c);
+  const int64_t few = T <= 1 ? 1 : T <= 2 ? 2 : T <= 4 ? 4 : kFewTokens, few_bytes = few * ((d + 15) / 16 * 16);
+  if (T <= kFewTokens && few_bytes <= kFewSmem) {
+    const FewParams p = {A, a_scale, B, b_scale, ldA, ldB, ldC, (int)T, (int)d, (int)V, c_dtype, C};
+    const int pr = prof_begin(c, 0);
+    auto stream = [&](auto kernel, int rows) {
+      int64_t blocks = (V + 16 * rows - 1) / (16 * rows);   // sixteen warps
+      if (blocks > (int64_t)c->n_sm * 2) blocks = (int64_t)c->n_sm * 2;
+      launch_smem(c, kernel, (int)blocks, 512, (size_t)few_bytes, p);
+    };
+    if (few == 1) stream(int8_few_kernel<1, 8>, 8);
+    else if (few == 2) stream(int8_few_kernel<2, 8>, 8);
+    else if (few == 4) stream(int8_few_kernel<4, 4>, 4);
+    else stream(int8_few_kernel<kFewTokens, 4>, 4);
+    prof_end(c, pr, 0);
+    c->launches++;
+    return cuda_ok();
+  }
+  const int cg = T <= BM ? 1 : c->cta_group;
+  CUtensorMap a, b;
+  if (!map_kmajor_i8(c, &a, A, (uint64_t)T, (uint64_t)d, (uint64_t)ldA, BM) ||
+      !map_kmajor_i8(c, &b, B, (uint64_t)V, (uint64_t)d, (uint64_t)ldB, b_box_rows(cg)))
+    return RL_ERR_CUDA;
+  GemmShape sh;
+  memset(&sh, 0, sizeof(sh));
+  sh.m_rows_cap = (int)T;
+  sh.k_cap = int8_k(d);
+  sh.n_tiles = (int)((V + BN - 1) / BN);
+  sh.n_split_max = sh.n_tiles;   // nothing is kept per column range
+  sh.m_group = row_group_tiles(c, (d + 1) / 2);
+  const ScaleParams p = {a_scale, b_scale, (int)V, C, ldC};
+  return c_dtype == RL_FP32 ? int8_tiles<kOutF32>(c, a, b, cg, sh, p, T)
+         : c_dtype == RL_FP16 ? int8_tiles<kOutF16>(c, a, b, cg, sh, p, T) : int8_tiles<kOutBf16>(c, a, b, cg, sh, p, T);
+}
+
+// Quantised rows of int8_linear in the workspace, their scales behind them.
+static inline size_t int8_rows_bytes(int64_t T, int64_t d) { return align_up((size_t)T * align_up((size_t)d, 16), 1024); }
+
+rl_status rl_workspace_bytes_int8_linear(rl_ctx* c, int64_t T, int64_t d, size_t* bytes) {
+  if (!c || !bytes || T < 0 || d <= 0) return RL_ERR_INVALID_ARG;
+  *bytes = int8_rows_bytes(T, d) + (size_t)T * 4;
+  return RL_OK;
+}
+
+rl_status rl_int8_linear(rl_ctx* c, const void* X, int x_dtype, int64_t ldX, const int8_t* B, int64_t ldB, const float* b_scale, int64_t T,
+                         int64_t d, int64_t V, void* C, int c_dtype, int64_t ldC) {
+  if (!c) return RL_ERR_INVALID_ARG;
+  rl_status s = check_int8(B, ldB, b_scale, T, d, V, C, c_dtype, ldC);
+  if (s != RL_OK) return s;
+  if (T > 0) {
+    if ((s = check_ws(c, int8_rows_bytes(T, d) + (size_t)T * 4)) != RL_OK) return s;
+  }
+  int8_t* A = static_cast<int8_t*>(c->ws);
+  float* a_scale = T > 0 ? reinterpret_cast<float*>(static_cast<char*>(c->ws) + int8_rows_bytes(T, d)) : nullptr;
+  const int64_t ldA = (int64_t)align_up((size_t)d, 16);
+  if ((s = rl_quantize_rows(c, X, x_dtype, ldX, T, d, A, ldA, a_scale)) != RL_OK || T == 0) return s;
+  return rl_int8_matmul(c, A, ldA, a_scale, B, ldB, b_scale, T, d, V, C, c_dtype, ldC);
+}
+
+rl_status rl_token_logprobs_int8(rl_ctx* c, const void* H, int64_t ldH, const int8_t* W, int64_t ldW, const float* w_scale,
+                                 const int32_t* tokens, const uint8_t* mask, int64_t T, int64_t d, int64_t V, float* logp,
+                                 float* entropy, float* lse) {
+  if (!c) return RL_ERR_INVALID_ARG;
+  rl_status s = check_hw(H, ldH, W, ldW, T, d, V);
+  if (s != RL_OK) return s;
+  if (d >= (1 << 17)) return RL_ERR_SHAPE;
+  if (ldW % 16 || (reinterpret_cast<uintptr_t>(w_scale) & 15)) return RL_ERR_ALIGNMENT;
+  if (T == 0) return RL_OK;
+  if (!tokens || !logp || !w_scale) return RL_ERR_INVALID_ARG;
+  const OnDevice on(c);
+  return score(c, H, ldH, W, ldW, w_scale, tokens, mask, T, d, V, logp, entropy, lse);
 }
 
 rl_status rl_policy_loss_shard_bwd(rl_ctx* c, const void* H, int64_t ldH, const void* W_shard, int64_t ldW,

@@ -4,6 +4,7 @@
 // conversion of dH.  All of them are bandwidth- or latency-bound; loads are coalesced and
 // vectorised where a row is wide enough to matter.
 #pragma once
+#include "int8_head.cuh"
 #include "logit_grad.cuh"
 
 namespace rlh {
@@ -183,8 +184,13 @@ struct PrepParams {
   const int* row_pos;     // read by the other
   RowOutputs out;
   unsigned* ticket;       // of the loss kernels that follow: cleared, whatever became of the call before
+  const float* H_scale;   // kRowsStored: of every row of H, which then points to 8-bit integers
+  float* scale_c;         // kRowsToInt8: of the compact rows, which then are 8-bit integers
 };
+// How rows become compact: as they are; from rows stored in 8 bits (int8_head.cuh) to the bf16 that those stand for; or from bf16 to 8 bits.
+enum RowKind { kRowsCopy = 0, kRowsStored = 1, kRowsToInt8 = 2 };
 
+template <int KIND>
 __device__ __forceinline__ void prep_row(const PrepParams& p, int t, int pos, int lane, DevStatus* st) {
   const int vec_per_row = p.d / 8;
   if (pos < 0) {
@@ -199,8 +205,19 @@ __device__ __forceinline__ void prep_row(const PrepParams& p, int t, int pos, in
   }
   uint4* dst = reinterpret_cast<uint4*>(p.Hc + (size_t)pos * p.d);
   const uint4* src = reinterpret_cast<const uint4*>(p.H + (size_t)t * p.ldH);
+  if constexpr (KIND == kRowsStored) {
+    const uint4* q = reinterpret_cast<const uint4*>(reinterpret_cast<const int8_t*>(p.H) + (size_t)t * p.ldH);
+    const float s = p.H_scale[t];
+#pragma unroll 4
+    for (int v = lane; v < p.d / 16; v += 32) unpack16(__ldg(q + v), s, dst[2 * v], dst[2 * v + 1]);
+  } else if constexpr (KIND == kRowsToInt8) {
+    uint2* q = reinterpret_cast<uint2*>(reinterpret_cast<int8_t*>(p.Hc) + (size_t)pos * p.d);
+    const float s = quantize_row_bf16(src, vec_per_row, q, lane);
+    if (lane == 0) p.scale_c[pos] = s;
+  } else {
 #pragma unroll 8
-  for (int v = lane; v < vec_per_row; v += 32) dst[v] = __ldg(src + v);
+    for (int v = lane; v < vec_per_row; v += 32) dst[v] = __ldg(src + v);
+  }
   if (lane == 0) {
     const int y = p.tokens[t];
     const bool in_range = y >= 0 && y < p.V;
@@ -212,7 +229,7 @@ __device__ __forceinline__ void prep_row(const PrepParams& p, int t, int pos, in
 // SCAN: every block counts the mask itself (the rows before its own, and all of them), up to kPrepRows rows: one launch
 // in place of three.  At 256 to 32768 rows the mask is 0.25 to 32 KB per block out of L2.
 constexpr int kPrepRows = 32768;
-template <bool SCAN>
+template <bool SCAN, int KIND>
 __global__ void __launch_bounds__(256) prep_rows_kernel(const PrepParams p, DevStatus* st) {
   chain_begin();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
@@ -247,15 +264,17 @@ __global__ void __launch_bounds__(256) prep_rows_kernel(const PrepParams p, DevS
     n = all_s;
     if (blockIdx.x == 0 && threadIdx.x == 0) st->n_valid = n;
     __syncthreads();
-    for (int i = warp; i < rows; i += warps) prep_row(p, r0 + i, pos_s[i], lane, st);
+    for (int i = warp; i < rows; i += warps) prep_row<KIND>(p, r0 + i, pos_s[i], lane, st);
   } else {
     n = st->n_valid;
-    for (int t = blockIdx.x * warps + warp; t < p.T; t += gridDim.x * warps) prep_row(p, t, p.row_pos[t], lane, st);
+    for (int t = blockIdx.x * warps + warp; t < p.T; t += gridDim.x * warps) prep_row<KIND>(p, t, p.row_pos[t], lane, st);
   }
   const int n_pad = (n + 127) / 128 * 128;
   for (int i = n + blockIdx.x * warps + warp; i < n_pad; i += gridDim.x * warps) {
-    uint4* dst = reinterpret_cast<uint4*>(p.Hc + (size_t)i * p.d);
-    for (int v = lane; v < p.d / 8; v += 32) dst[v] = make_uint4(0, 0, 0, 0);
+    constexpr int kBytes = KIND == kRowsToInt8 ? 1 : 2;
+    uint4* dst = reinterpret_cast<uint4*>(reinterpret_cast<char*>(p.Hc) + (size_t)i * p.d * kBytes);
+    for (int v = lane; v < p.d * kBytes / 16; v += 32) dst[v] = make_uint4(0, 0, 0, 0);
+    if (KIND == kRowsToInt8 && lane == 0) p.scale_c[i] = 0.f;
     if (lane == 0) p.tokens_c[i] = -1;
   }
 }
@@ -747,6 +766,10 @@ struct LossParams {
   int slab_cap, slab_one, slab_index;
   uint4* clear;            // ticket and counters of the gradient jobs that follow
   int n_clear;
+  // cross entropy (its own instantiation): (1 - smooth) (lse - z_y) + smooth (lse - mean z) + z_coef lse^2
+  float smooth, z_coef;
+  int V;
+  float* each_out;         // [T], the loss of every token before its weight, or NULL
 };
 // Fixed-order sum of column k of the block partials by one warp: lane l adds blocks l, l + 32, ... in order, then a
 // butterfly over the lanes; the order depends on n_blocks alone, so the result is reproducible.
@@ -811,7 +834,9 @@ __device__ __forceinline__ void finish_loss(const double (&acc)[kLossSums], cons
 // few: with one thread per row a call of a few hundred rows and 75 to 148 ranges was a chain of that many loads, 17 us.
 // kW = 1 where there are rows enough to fill the machine, and where there is nothing to merge (merge_by_thread).
 // CLEAR: the counters of gradient jobs that follow are cleared in passing.
-template <int kW, bool CLEAR>
+// CE: the cross entropy from statistics whose third is sum z (RowStatsOf<true>).  Metrics: weighted sums of lse - z_y, of lse - mean z, of
+// lse^2, of the tokens whose logit is the row's largest, of lse; the largest lse - z_y.
+template <int kW, bool CLEAR, bool CE = false>
 __global__ void __launch_bounds__(kLossThreads) combine_loss_kernel(const LossParams p, DevStatus* st) {
   chain_begin();
   constexpr int kTeams = kLossThreads / 32 / kW;
@@ -841,7 +866,9 @@ __global__ void __launch_bounds__(kLossThreads) combine_loss_kernel(const LossPa
     float A_t = 0.f, old_lp = 0.f, ref_lp = 0.f, tw = 0.f;
     if (warp == 0 && in) {
       row = p.row_map[i];
-      if (p.with_loss) {
+      if (CE) {
+        if (p.token_weight) tw = p.token_weight[row];
+      } else if (p.with_loss) {
         A_t = p.adv[row];
         old_lp = p.old_logp[row];
         if (p.token_weight) tw = p.token_weight[row];
@@ -861,7 +888,7 @@ __global__ void __launch_bounds__(kLossThreads) combine_loss_kernel(const LossPa
         const float4 q = q1[(size_t)r * p.part_stride];
         const float m = fmaxf(M, q.x), a = exp2f((M - m) * kLog2e), b = exp2f((q.x - m) * kLog2e);
         S = fmaf(S, a, q.y * b);
-        A = fmaf(A, a, q.z * b);
+        A = CE ? A + q.z : fmaf(A, a, q.z * b);
         zy += q.w;
         if (p.kl_full) {
           const float4 k = q2[(size_t)r * p.part_stride];
@@ -896,7 +923,7 @@ __global__ void __launch_bounds__(kLossThreads) combine_loss_kernel(const LossPa
         for (int w = 0; w < kW; ++w) {
           const float m = ps[0][w][lane], b = m == -CUDART_INF_F ? 0.f : exp2f((m - Mt) * kLog2e);   // -inf: no range
           S = fmaf(ps[1][w][lane], b, S);
-          A = fmaf(ps[2][w][lane], b, A);
+          A = CE ? A + ps[2][w][lane] : fmaf(ps[2][w][lane], b, A);
           zy += ps[3][w][lane];
           if (p.kl_full) {
             const float mr = ps[5][w][lane];
@@ -914,7 +941,7 @@ __global__ void __launch_bounds__(kLossThreads) combine_loss_kernel(const LossPa
       }
       lse = M + logf(S);
       logp = zy - lse;
-      ent = lse - A / S;
+      ent = CE ? 0.f : lse - A / S;
     }
     if (p.kl_full) {
       const float lse_ref = Mr + logf(Sr);
@@ -924,13 +951,27 @@ __global__ void __launch_bounds__(kLossThreads) combine_loss_kernel(const LossPa
     }
     if (p.kl_out) p.kl_out[row] = kl;
     p.lse_c[i] = lse;
-    p.ent_c[i] = ent;
+    if (!CE) p.ent_c[i] = ent;
     if (p.logp_c) p.logp_c[i] = logp;
     if (p.logp_out) p.logp_out[row] = logp;
     if (p.ent_out) p.ent_out[row] = ent;
     if (p.lse_out) p.lse_out[row] = lse;
     if (p.zero_coef) p.cp_c[i] = p.ce_c[i] = 0.f;
-    if (p.with_loss) {
+    if constexpr (CE) {
+      const float w = p.token_weight ? tw : w_mean;
+      const float uniform = lse - A / (float)p.V;
+      const float each = fmaf(p.z_coef * lse, lse, fmaf(1.f - p.smooth, -logp, p.smooth * uniform));
+      if (p.each_out) p.each_out[row] = each;
+      p.cp_c[i] = w * fmaf(2.f * p.z_coef, lse, 1.f);
+      p.ce_c[i] = w * (1.f - p.smooth);
+      acc[0] += (double)w * (double)each;
+      acc[1] += (double)w * (double)(-logp);
+      acc[2] += (double)w * (double)uniform;
+      acc[3] += (double)w * (double)lse * (double)lse;
+      acc[4] += zy >= M ? (double)w : 0.0;
+      acc[5] += (double)w * (double)lse;
+      acc[6] = fmax(acc[6], (double)(-logp));
+    } else if (p.with_loss) {
       const float w = p.token_weight ? tw : w_mean;
       const float rho = expf(logp - old_lp);
       const float clipped = fminf(fmaxf(rho, 1.f - p.eps_low), 1.f + p.eps_high);
@@ -1381,8 +1422,8 @@ __global__ void __launch_bounds__(256) scatter_dH_kernel(const DhSource s, const
 }
 
 // dW of one slab; extra warps write dH of the same slab, which the launch before has left, meanwhile: a launch less.
-template <int W>
-struct EpiAccScatter : EpiAccW<W> {
+template <int W, bool HALF = false>
+struct EpiAccScatter : EpiAccW<W, HALF> {
   static constexpr int kSideWarps = 4;
   struct Params : AccParams {
     DhSource dh;

@@ -1,0 +1,273 @@
+"""Rows in 8 bits, their products and scoring under a head held in 8 bits, against their definitions: integers and scales exactly,
+products to the roundings that the definition names."""
+import pytest
+import torch
+
+from tests.head_reference import HALF_STEP, assert_within, quantize_rows
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = [torch.bfloat16, torch.float16, torch.float32]
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    from paper_2512_21450_b200 import Context
+    c = Context(0)
+    yield c
+    c.close()
+
+
+def _rows(T, d, dtype, seed=0, std=1.0):
+    g = torch.Generator(DEV).manual_seed(seed)
+    return (torch.randn(T, d, generator=g, device=DEV) * std).to(dtype)
+
+
+def _ok(ctx):
+    s, detail = ctx.last_device_status()
+    assert s == 0, (s, hex(detail))
+
+
+# ------------------------------------------------------------------ quantised rows
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,d", [(1, 1), (3, 7), (5, 16), (9, 255), (64, 1000), (33, 2048), (17, 2056), (1000, 3584), (4, 70001)])
+def test_rows_exactly(ctx, dtype, T, d):
+    x = _rows(T, d, dtype, seed=T + d)
+    Q, s = ctx.rl_quantize_rows(x)
+    q, scale = quantize_rows(x)
+    assert torch.equal(Q.double(), q) and torch.equal(s, scale)
+    assert Q.stride(0) % 16 == 0 or T == 1
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_ties_and_signs(ctx, dtype):
+    """Multiples of halves of a row whose largest is 127: products that lie exactly between two integers go to the even one."""
+    x = torch.arange(-127, 127.5, 0.5, device=DEV)[None].to(dtype)
+    Q, s = ctx.rl_quantize_rows(x)
+    assert s.item() == 1.0 and torch.equal(Q.double(), torch.round(x.double()))
+    q, _ = quantize_rows(x * 3)
+    assert torch.equal(ctx.rl_quantize_rows(x * 3)[0].double(), q)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rows_of_zeros_and_what_is_not_finite(ctx, dtype):
+    x = _rows(8, 100, dtype)
+    x[0] = 0
+    x[1, 17] = float("inf")
+    x[2, 99] = float("nan")
+    x[3, 0] = float("-inf")
+    x[4] = 0
+    x[4, 5] = -0.0
+    x[5] = 2.0 ** -24                       # a subnormal fp16
+    x[6] = torch.finfo(dtype).max
+    Q, s = ctx.rl_quantize_rows(x)
+    q, scale = quantize_rows(x)
+    assert torch.equal(Q.double(), q) and torch.equal(s.nan_to_num(-1), scale.nan_to_num(-1))
+    assert s[0] == 0 and s[4] == 0 and bool(torch.isnan(s[1:4]).all()) and bool((Q[:5] == 0).all())
+    assert bool((Q[5] == 127).all()) and bool((Q[6] == 127).all())
+    if dtype != torch.float16:
+        tiny = torch.tensor([[2.0 ** -100, -2.0 ** -101], [2.0 ** -101, 0.0]], device=DEV).to(dtype)
+        Q, s = ctx.rl_quantize_rows(tiny)
+        assert Q.tolist() == [[127, -64], [0, 0]] and s[1] == 0 and s[0] > 0
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rows_with_strides_and_what_lies_around_them(ctx, dtype):
+    wide = _rows(20, 130, dtype, seed=3)
+    x = wide[:, 1:98]                       # rows that start anywhere
+    Q = torch.full((20, 112), -99, dtype=torch.int8, device=DEV)
+    s = torch.empty(20, device=DEV)
+    ctx.rl_quantize_rows(x, Q=Q[:, :97], scale=s)
+    q, scale = quantize_rows(x)
+    assert torch.equal(Q[:, :97].double(), q) and torch.equal(s, scale) and bool((Q[:, 97:] == -99).all())
+    assert ctx.rl_quantize_rows(x[:0])[0].shape == (0, 97)
+
+
+# ------------------------------------------------------------------ products
+def _product(A, a, B, b):
+    """Exact sums, rounded to fp32, times a, times b (fp32), before the last rounding."""
+    n = A.double() @ B.double().T          # below 2^53
+    return n.float() * a[:, None] * b[None, :], n
+
+
+def _int8(T, d, seed, lo=-128):
+    g = torch.Generator(DEV).manual_seed(seed)
+    ld = (d + 15) // 16 * 16
+    x = torch.full((T, ld), 111, dtype=torch.int8, device=DEV)   # behind the rows: what must not count
+    x[:, :d] = torch.randint(lo, 128, (T, d), generator=g, device=DEV, dtype=torch.int8)
+    return x[:, :d], torch.rand(T, generator=g, device=DEV) + 0.5
+
+
+PRODUCTS = [(1, 1, 1), (1, 64, 7), (2, 17, 33), (3, 2048, 1000), (4, 100, 515), (5, 33, 2), (8, 1000, 4099), (7, 8000, 300), (8, 8192, 77),
+            (8, 8193, 65), (9, 64, 1), (9, 1, 300), (16, 129, 256), (128, 256, 1000), (129, 256, 1000), (200, 1000, 4099), (300, 2048, 513), (257, 127, 8)]
+
+
+@pytest.mark.parametrize("T,d,V", PRODUCTS)
+@pytest.mark.parametrize("out", TYPES)
+def test_product_exactly(ctx, T, d, V, out):
+    (A, a), (B, b) = _int8(T, d, T + d), _int8(V, d, V + d + 1)
+    want, _ = _product(A, a, B, b)
+    C = torch.full((T, V), float("nan"), dtype=out, device=DEV)
+    got = ctx.rl_int8_matmul(A, a, B, b, out_dtype=out, out=C)
+    _ok(ctx)
+    assert torch.equal(got, want.to(out))
+
+
+@pytest.mark.parametrize("T", [2, 40, 300])
+@pytest.mark.parametrize("out", TYPES)
+@pytest.mark.parametrize("V,ld,at", [(500, 520, 0), (500, 512, 3), (257, 259, 1), (64, 64, 0)])
+def test_product_into_a_part_of_a_matrix(ctx, T, out, V, ld, at):
+    (A, a), (B, b) = _int8(T, 200, 1), _int8(V, 200, 2)
+    big = torch.full((T + 1, ld + at), 5.0, dtype=out, device=DEV)
+    C = big[:T, at:at + V]
+    ctx.rl_int8_matmul(A, a, B, b, out_dtype=out, out=C)
+    _ok(ctx)
+    assert torch.equal(C, _product(A, a, B, b)[0].to(out))
+    assert bool((big[T] == 5).all()) and bool((big[:, :at] == 5).all()) and bool((big[:, at + V:] == 5).all())
+
+
+@pytest.mark.parametrize("T", [1, 8, 9, 130])
+def test_largest_sums(ctx, T):
+    """Every product the largest there is: sums up to 2^31 - 2^14."""
+    d = (1 << 17) - 1
+    A = torch.full((T, d + 1), -128, dtype=torch.int8, device=DEV)[:, :d]
+    B = torch.full((20, d + 1), -128, dtype=torch.int8, device=DEV)[:, :d]
+    B[3] = 127
+    one = torch.ones(T, device=DEV)
+    got = ctx.rl_int8_matmul(A, one, B, torch.ones(20, device=DEV), out_dtype=torch.float32)
+    _ok(ctx)
+    want = torch.full((T, 20), float(128 * 128 * d), device=DEV)
+    want[:, 3] = float(-128 * 127 * d)
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("x_dtype", TYPES)
+@pytest.mark.parametrize("T,d,V", [(1, 2048, 1001), (6, 100, 300), (33, 1000, 4099), (300, 512, 777)])
+def test_linear(ctx, x_dtype, T, d, V):
+    X, W = _rows(T, d, x_dtype, seed=1), _rows(V, d, torch.bfloat16, seed=2, std=0.05)
+    Wq, ws = ctx.rl_quantize_rows(W)
+    got = ctx.rl_int8_linear(X, Wq, ws, out_dtype=torch.float32)
+    _ok(ctx)
+    q, s = quantize_rows(X)
+    assert torch.equal(got, _product(q, s, Wq, ws)[0])
+    # and near the product that it stands for: every q is half an integer off at most
+    exact = X.double() @ W.double().T
+    qa, qw = s.double()[:, None] / 2, ws.double()[None, :] / 2
+    bound = qa * W.double().abs().sum(1)[None, :] + qw * X.double().abs().sum(1)[:, None] + qa * qw * d
+    assert_within(got, exact, bound * 1.001, "logits")
+
+
+def test_nan_and_zero_tokens(ctx):
+    for T in (4, 20):
+        X, W = _rows(T, 128, torch.bfloat16, seed=5), _rows(300, 128, torch.bfloat16, seed=6)
+        X[1, 3] = float("inf")
+        X[2] = 0
+        Wq, ws = ctx.rl_quantize_rows(W)
+        out = ctx.rl_int8_linear(X, Wq, ws)
+        assert bool(torch.isnan(out[1]).all()) and bool((out[2] == 0).all()) and bool(torch.isfinite(out[0]).all())
+    assert ctx.rl_int8_linear(X[:0], Wq, ws).shape == (0, 300)
+
+
+def test_half_precision_overflows_to_infinity(ctx):
+    A = torch.full((2, 64), 127, dtype=torch.int8, device=DEV)
+    out = ctx.rl_int8_matmul(A, torch.ones(2, device=DEV), A, torch.ones(2, device=DEV), out_dtype=torch.float16)
+    assert bool(torch.isinf(out).all())
+
+
+def test_offsets_past_32_bits(ctx):
+    """More than 2^31 logits, and a B of more than 2^31 bytes."""
+    T, V, d = 16384, 151936, 16
+    (A, a), (B, b) = _int8(T, d, 3), _int8(V, d, 4)
+    C = torch.empty(T, V, dtype=torch.bfloat16, device=DEV)
+    ctx.rl_int8_matmul(A, a, B, b, out=C)
+    _ok(ctx)
+    for t in (0, 14000, T - 1):
+        assert torch.equal(C[t], _product(A[t:t + 1], a[t:t + 1], B, b)[0][0].bfloat16())
+    odd = torch.empty(T * V + 8, dtype=torch.bfloat16, device=DEV)[1:1 + T * V].view(T, V)   # not through the TMA unit
+    ctx.rl_int8_matmul(A, a, B, b, out=odd)
+    assert torch.equal(odd, C)
+    del C, odd
+    V, ld = 200000, 16384
+    big = torch.empty(V, ld, dtype=torch.int8, device=DEV)
+    big[:, :64] = torch.randint(-128, 128, (V, 64), device=DEV, dtype=torch.int8)
+    b = torch.rand(V, device=DEV)
+    for T in (2, 20):
+        A, a = _int8(T, 64, 5)
+        got = ctx.rl_int8_matmul(A, a, big[:, :64], b, out_dtype=torch.float32)
+        assert torch.equal(got, _product(A, a, big[:, :64], b)[0])
+
+
+def test_streams_and_graphs(ctx):
+    X, W = _rows(5, 512, torch.bfloat16, seed=7), _rows(1000, 512, torch.bfloat16, seed=8)
+    Wq, ws = ctx.rl_quantize_rows(W)
+    out = ctx.rl_int8_linear(X, Wq, ws)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        again = ctx.rl_int8_linear(X, Wq, ws)
+    side.synchronize()
+    assert torch.equal(again, out)
+    C = torch.empty_like(out)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ctx.rl_int8_linear(X, Wq, ws, out=C)
+    X2 = _rows(5, 512, torch.bfloat16, seed=9)
+    X.copy_(X2)
+    graph.replay()
+    torch.cuda.synchronize()
+    got = C.clone()
+    assert torch.equal(got, ctx.rl_int8_linear(X2, Wq, ws))
+
+
+# ------------------------------------------------------------------ scoring
+@pytest.mark.parametrize("T,d,V", [(1, 64, 1), (1, 64, 300), (77, 192, 1000), (128, 2048, 3000), (129, 1024, 777), (700, 2176, 1500), (2000, 256, 5000)])
+def test_scoring(ctx, T, d, V):
+    g = torch.Generator(DEV).manual_seed(T + d)
+    W = _rows(V, d, torch.bfloat16, seed=1, std=0.05)
+    tok = torch.randint(0, V, (T,), generator=g, device=DEV, dtype=torch.int32)
+    H = (_rows(T, d, torch.float32, seed=2) + 6 * torch.rand(T, 1, generator=g, device=DEV) / (0.0025 * d) * W[tok.long()].float()).bfloat16()
+    mask = (torch.rand(T, generator=g, device=DEV) < 0.7).to(torch.uint8) if T > 1 else None
+    if mask is not None:
+        H[mask == 0] = float("nan")
+        tok[mask == 0] = -5
+    Wq, ws = ctx.rl_quantize_rows(W)
+    logp, ent, lse = ctx.rl_token_logprobs_int8(H, Wq, ws, tok, mask)
+    _ok(ctx)
+    on = torch.ones(T, dtype=torch.bool, device=DEV) if mask is None else mask != 0
+    q, s = quantize_rows(H[on])
+    z = (q @ Wq.double().T) * s.double()[:, None] * ws.double()
+    dz = 3 * HALF_STEP[torch.float32] * z.abs().amax(1)              # one rounding, two multiplications
+    L = torch.logsumexp(z, 1)
+    lp = z - L[:, None]
+    dL = dz + 1e-6 * (L.abs() + 12)
+    assert_within(lse[on], L, dL, "lse")
+    assert_within(logp[on], lp.gather(1, tok[on].long()[:, None])[:, 0], dz + dL, "logp")
+    p = lp.exp()
+    E = -(p * lp).sum(1)
+    # lse - sum p z, the sum with weights off by 2 (dz + 1e-6) at most
+    assert_within(ent[on], E, dL + (p * z.abs()).sum(1) * 4 * (dz + 1e-6) + dz, "entropy")
+    for x in (logp, ent, lse):
+        assert bool((x[~on] == 0).all())
+
+
+def test_scoring_agrees_with_the_logits(ctx):
+    """The stages as they are used together: quantised head, logits of a prompt, scores of its tokens."""
+    W = _rows(2000, 512, torch.bfloat16, seed=1, std=0.05)
+    H = _rows(300, 512, torch.bfloat16, seed=2)
+    tok = torch.randint(0, 2000, (300,), device=DEV, dtype=torch.int32)
+    Wq, ws = ctx.rl_quantize_rows(W)
+    z = ctx.rl_int8_linear(H, Wq, ws, out_dtype=torch.float32).double()
+    logp, _, lse = ctx.rl_token_logprobs_int8(H, Wq, ws, tok)
+    assert (lse - torch.logsumexp(z, 1)).abs().max().item() <= 1e-6 * 20
+    assert (logp - torch.log_softmax(z, 1).gather(1, tok.long()[:, None])[:, 0]).abs().max().item() <= 1e-6 * 40
+    few = torch.cat([ctx.rl_int8_linear(H[i:i + 5], Wq, ws, out_dtype=torch.float32) for i in range(0, 300, 5)])
+    assert torch.equal(few.double(), z)       # one path or the other, the same numbers
+    # scored states of a rollout stored in 8 bits, then a supervised step on them
+    Q, s = ctx.rl_quantize_rows(H)
+    out = ctx.rl_cross_entropy_fwd_bwd(Q, W, tok, H_scale=s)
+    assert torch.equal(ctx.rl_int8_matmul(Q, s, Wq, ws, out_dtype=torch.float32).double(), z)
+    assert (out["logp"] - logp).abs().mean().item() < 0.1 and _isfinite(out)
+
+
+def _isfinite(out):
+    return all(bool(torch.isfinite(v).all()) for v in out.values())
