@@ -474,6 +474,8 @@ struct UnitWalk {
 //     static constexpr bool kAhead;                            // State has next_row and next_col: this warp's first row and column of the next tile
 //     static constexpr int kSideWarps; static constexpr bool kFeeds; };   // if kSideWarps > 0:
 //     static void side(const Params&, const GemmExtents&, int cg, int n_workers, int warp);
+//   if kInt8, before the accumulator of a tile is waited for; chunk0: this warp's first chunk, next: the unit's next tile or -1:
+//     static void begin_tile(const Params&, State&, int n_tile, int next, int chunk0);
 //     static constexpr bool kInt8;                             // 8-bit integer operands (K-major): chunks are the bits of 32-bit integers
 //   if kFeeds:
 //     static bool feeds(const Params&, const GemmExtents&, int n_workers);   // or A is complete when the launch starts
@@ -792,6 +794,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
       }
       for (int n = n0; n < n1 && ok; ++n, t += has_k ? 1u : 0u) {
         const uint32_t a = MODE == kTileSquare ? (t & 1u) : 0u;
+        if constexpr (Epi::kInt8) Epi::begin_tile(ep, st, n, n + 1 < n1 ? n + 1 : -1, half * kChunks);
         if (has_k) {
           const uint32_t par = MODE == kTileSquare ? ((t >> 1) & 1u) : (t & 1u);
           if (!mbar_wait_bounded_cluster(smem_u32(&bar_acc_full[a]), par, abort_p)) {

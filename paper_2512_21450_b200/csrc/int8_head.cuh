@@ -100,7 +100,9 @@ __device__ __forceinline__ void load8(const T* row, int64_t k, int64_t d, float 
 template <class T, bool VEC>
 __global__ void __launch_bounds__(256) quantize_rows_kernel(const T* X, int64_t ldX, int64_t rows, int64_t d, int8_t* Q, int64_t ldQ,
                                                             float* scale) {
-  chain_begin();
+  // released once everything before is done: a product that follows may read its other operand at once (StreamParams::early)
+  chain_wait();
+  chain_release();
   const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
   for (int64_t r = (int64_t)blockIdx.x * warps + (threadIdx.x >> 5); r < rows; r += (int64_t)gridDim.x * warps) {
     const T* src = X + r * ldX;
@@ -135,27 +137,58 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const T* X, int64_t 
 }
 
 // ---------------------------------------------------------------------------------------------
-// 32 integer sums of one row -> logits.  b: scales of columns from col0 on, 16-byte aligned at multiples of 4.
-__device__ __forceinline__ void scale_chunk(const float (&v)[32], float a, const float* b, int nvalid, float (&z)[32]) {
-  if (nvalid >= 32) {
+// Scales of a warp's columns.  Lane i holds those of columns i of the warp's chunks of a tile, and of the unit's next tile, loaded before
+// the accumulator is waited for: while the ring streams B, a load takes microseconds even where it hits L2 (a uniform load per four
+// columns at each chunk made a 128 x 256 tile's epilogue 13 us).  Every chunk's 32 then go through shared memory to all lanes.
+template <int W>
+struct ColumnScales {
+  static constexpr int kChunks = BN / 32 / (W / 4);
+  float now[kChunks], ahead[kChunks];
+  int tile_ahead;   // whose scales `ahead` has
+  __device__ __forceinline__ void init() { tile_ahead = -1; }
+  __device__ __forceinline__ void load(float (&x)[kChunks], const float* b, int V, int n_tile, int chunk0) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) {
+      const int col = n_tile * BN + (chunk0 + i) * 32 + lane;
+      x[i] = col < V ? __ldg(b + col) : 0.f;
+    }
+  }
+  __device__ __forceinline__ void begin_tile(const float* b, int V, int n_tile, int next, int chunk0) {
+    if (tile_ahead == n_tile) {
+#pragma unroll
+      for (int i = 0; i < kChunks; ++i) now[i] = ahead[i];
+    } else {
+      load(now, b, V, n_tile, chunk0);
+    }
+    if (next >= 0) load(ahead, b, V, next, chunk0);
+    tile_ahead = next;
+  }
+  // 32 integer sums of one row, whose scale is a -> logits; columns past V become 0.  Chunks come in order.
+  __device__ __forceinline__ void apply(const float (&v)[32], float a, float (&z)[32]) {
+    __shared__ __align__(16) float scale_s[W][32];
+    const int lane = threadIdx.x & 31;
+    float* mine = scale_s[(threadIdx.x >> 5) - 2];
+    __syncwarp();   // the chunk before has been read
+    mine[lane] = now[0];
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i + 1 < kChunks; ++i) now[i] = now[i + 1];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float4 q = __ldg(reinterpret_cast<const float4*>(b) + j);
+      const float4 q = reinterpret_cast<const float4*>(mine)[j];
       z[4 * j] = (float)__float_as_int(v[4 * j]) * a * q.x;
       z[4 * j + 1] = (float)__float_as_int(v[4 * j + 1]) * a * q.y;
       z[4 * j + 2] = (float)__float_as_int(v[4 * j + 2]) * a * q.z;
       z[4 * j + 3] = (float)__float_as_int(v[4 * j + 3]) * a * q.w;
     }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 32; ++i) z[i] = i < nvalid ? (float)__float_as_int(v[i]) * a * __ldg(b + i) : 0.f;
   }
-}
+};
 
 // Statistics of RowStats over those logits: scoring under a head held in 8 bits.
 struct Int8StatsParams : RowStats::Params {
   const float* row_scale;   // compact rows
-  const float* col_scale;   // [V], 16-byte aligned
+  const float* col_scale;   // [V]
 };
 template <int W>
 struct EpiStatsI8 {
@@ -167,9 +200,13 @@ struct EpiStatsI8 {
   using Params = Int8StatsParams;
   struct State : RowStats::State {
     float scale;
+    ColumnScales<W> cols;
   };
-  __device__ static __forceinline__ void init(State&) {}
+  __device__ static __forceinline__ void init(State& st) { st.cols.init(); }
   __device__ static __forceinline__ void finish(State&) {}
+  __device__ static __forceinline__ void begin_tile(const Params& p, State& st, int n_tile, int next, int chunk0) {
+    st.cols.begin_tile(p.col_scale, p.V, n_tile, next, chunk0);
+  }
   __device__ static __forceinline__ void begin_unit(const Params& p, State& st, int m_tile, int nr, int row_in_tile, int m_rows,
                                                     int slab_off, int ks) {
     RowStats::begin_unit(p, st, m_tile, nr, row_in_tile, m_rows, slab_off, ks);
@@ -178,10 +215,8 @@ struct EpiStatsI8 {
   }
   __device__ static __forceinline__ void chunk(const Params& p, State& st, int m_tile, int n_tile, int c, int row_in_tile, int m_rows,
                                                const float (&v)[32], const CUtensorMap* map, uint32_t staging) {
-    const int col0 = n_tile * BN + c * 32;
-    if (col0 >= p.V) return;
     float z[32];
-    scale_chunk(v, st.scale, p.col_scale + col0, p.V - col0, z);
+    st.cols.apply(v, st.scale, z);
     RowStats::chunk(p, st, m_tile, n_tile, c, row_in_tile, m_rows, z, map, staging);
   }
   static constexpr int kMerge = RowStats::kMerge;
@@ -213,7 +248,7 @@ __device__ __forceinline__ void store_one(void* C, size_t at, float x) {
 }
 struct ScaleParams {
   const float* row_scale;
-  const float* col_scale;   // 16-byte aligned
+  const float* col_scale;
   int V;
   void* C;                  // not TMA
   long long ldC;
@@ -230,8 +265,15 @@ struct EpiScale {
   struct State {
     float scale;
     uint32_t n_issued;
+    ColumnScales<W> cols;
   };
-  __device__ static __forceinline__ void init(State& st) { st.n_issued = 0; }
+  __device__ static __forceinline__ void init(State& st) {
+    st.n_issued = 0;
+    st.cols.init();
+  }
+  __device__ static __forceinline__ void begin_tile(const Params& p, State& st, int n_tile, int next, int chunk0) {
+    st.cols.begin_tile(p.col_scale, p.V, n_tile, next, chunk0);
+  }
   __device__ static __forceinline__ void finish(State& st) {
     if ((threadIdx.x & 31) == 0 && st.n_issued) bulk_wait_group_all();
     __syncwarp();
@@ -247,7 +289,7 @@ struct EpiScale {
     constexpr bool kPairs = TMA && OUT != kOutF32;   // a box holds two chunks: its second half may lie past V, and is clipped
     if (row0 >= m_rows || (kPairs ? col0 & ~63 : col0) >= p.V) return;   // warp-uniform
     float z[32];
-    scale_chunk(v, st.scale, p.col_scale + col0, p.V - col0, z);
+    st.cols.apply(v, st.scale, z);
     constexpr int kBufs = kStagingBytes / kWarps / kBoxBytes;
     if constexpr (kPairs) {
       uint32_t w[16];
@@ -292,98 +334,201 @@ struct EpiScale {
 };
 
 // ---------------------------------------------------------------------------------------------
-// A few tokens: a stream of B.  A warp takes kRows rows of B at a time, 16 bytes of each per lane and step, and multiplies them with the
-// tokens, which lie in shared memory; the sums over the lanes are formed by halving, so that every lane ends up with one of them.
-constexpr int kFewTokens = 8;
-constexpr int kFewSmem = 64 * 1024;
-struct FewParams {
-  const int8_t* A;
-  const float* a_scale;
-  const int8_t* B;
-  const float* b_scale;
-  long long ldA, ldB, ldC;
-  int T, d, V, out;
-  void* C;
-};
-__device__ __forceinline__ int dot16(const uint4& a, const uint4& b, int acc) {
-  acc = __dp4a((int)a.x, (int)b.x, acc);
-  acc = __dp4a((int)a.y, (int)b.y, acc);
-  acc = __dp4a((int)a.z, (int)b.z, acc);
-  return __dp4a((int)a.w, (int)b.w, acc);
+// Up to N tokens as a stream of B on the tensor cores, the operands' roles exchanged: 128 rows of B are the M side of a tile, the tokens
+// its N side.  All of the tokens lie in shared memory for the whole kernel.  (As the M side of the engine's tiles they were read again
+// for every tile by every CTA, which made the L2 slices of a few lines the bottleneck: 9 to 32 tokens took 110 to 140 us at
+// d = 3584 and 152 K rows, 40 to 128 took 97 to 101; a dp4a kernel took 95 us for one token and 139 for eight.)  Every CTA takes an equal share of the rows in tiles of `rows`.
+//   warp 0: TMA producer;  warp 1: allocates tensor memory, issues the products;  warps 2 to 5: a thread per row of B.
+constexpr int kStreamStageBytes = 128 * 128;   // 128 rows, a k-block of 128 bytes
+constexpr int kStreamMaxStages = 12, kStreamMinStages = 4;
+constexpr int kStreamSmem = 224 * 1024;        // of it 1 KB to start on a multiple of 1024
+constexpr int kStreamThreads = 192;
+// Stages that fit beside the tokens; fewer than kStreamMinStages: too many tokens for this kernel.
+__host__ __device__ constexpr int stream_stages(int n_tokens, int k_blocks) {
+  const long long left = kStreamSmem - 1024 - (long long)n_tokens * 128 * k_blocks;
+  const long long s = left < 0 ? 0 : left / kStreamStageBytes;
+  return (int)(s < kStreamMaxStages ? s : kStreamMaxStages);
 }
-template <int T, int R>
-__global__ void __launch_bounds__(512) int8_few_kernel(const FewParams p) {
-  chain_begin();
-  extern __shared__ __align__(16) uint8_t few_smem[];
-  const int vecs = (p.d + 15) / 16;
-  uint4* x_s = reinterpret_cast<uint4*>(few_smem);   // [T][vecs], zero past d and past the tokens there are
-  for (int i = threadIdx.x; i < T * vecs; i += blockDim.x) {
-    const int t = i / vecs, v = i - t * vecs;
-    uint4 q = make_uint4(0, 0, 0, 0);
-    if (t < p.T) {
-      const int8_t* src = p.A + t * p.ldA + v * 16;
-      if (v * 16 + 16 <= p.d) {
-        q = *reinterpret_cast<const uint4*>(src);
-      } else {
-        uint32_t w[4] = {0, 0, 0, 0};
-        for (int k = 0; v * 16 + k < p.d; ++k) w[k / 4] |= (uint32_t)(uint8_t)src[k] << (8 * (k & 3));
-        q = make_uint4(w[0], w[1], w[2], w[3]);
-      }
-    }
-    x_s[i] = q;
+struct StreamParams {
+  const float* a_scale;
+  const float* b_scale;
+  int T, V, k_blocks, rows, stages;   // rows of B per tile, at most 128
+  int early;   // the launch before this one is quantize_rows_kernel: whatever wrote B is done, and its first tiles are fetched meanwhile
+  void* C;
+  long long ldC;
+};
+template <int N, int OUT>
+__global__ void __launch_bounds__(kStreamThreads, 1)
+int8_stream_kernel(const __grid_constant__ CUtensorMap tmTokens, const __grid_constant__ CUtensorMap tmRows, const StreamParams p, DevStatus* status) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) uint64_t bar_full[kStreamMaxStages], bar_empty[kStreamMaxStages], bar_acc_full[2], bar_acc_empty[2], bar_tokens, bar_drain;
+  __shared__ uint32_t tmem_base_smem;
+  __shared__ int abort_flag;
+  __shared__ float a_s[4][N];   // a copy per warp
+  constexpr uint32_t kCols = 2 * N;   // two accumulators; a power of two from 32 on
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t tokens = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t ring = tokens + (uint32_t)p.k_blocks * N * 128u;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStreamMaxStages; ++s) { mbar_init(smem_u32(&bar_full[s]), 1); mbar_init(smem_u32(&bar_empty[s]), 1); }
+    for (int a = 0; a < 2; ++a) { mbar_init(smem_u32(&bar_acc_full[a]), 1); mbar_init(smem_u32(&bar_acc_empty[a]), 4); }
+    mbar_init(smem_u32(&bar_tokens), 1);
+    mbar_init(smem_u32(&bar_drain), 1);
+    abort_flag = 0;
+    fence_mbar_init();
+    prefetch_tmap(&tmTokens);
+    prefetch_tmap(&tmRows);
   }
+  if (warp == 1) {
+    tmem_alloc(smem_u32(&tmem_base_smem), kCols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
   __syncthreads();
-  const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-  const int groups = (p.V + R - 1) / R;
-  for (int g = blockIdx.x * warps + (threadIdx.x >> 5); g < groups; g += gridDim.x * warps) {
-    const int v0 = g * R;
-    int n[R * T];   // sum of (row r, token t) at r * T + t
-#pragma unroll
-    for (int i = 0; i < R * T; ++i) n[i] = 0;
-    const uint4* row[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) row[r] = reinterpret_cast<const uint4*>(p.B + (long long)min(v0 + r, p.V - 1) * p.ldB);
-#pragma unroll 2
-    for (int k = lane; k < vecs; k += 32) {
-      uint4 w[R];
-#pragma unroll
-      for (int r = 0; r < R; ++r) w[r] = __ldcs(row[r] + k);
-#pragma unroll
-      for (int t = 0; t < T; ++t) {
-        const uint4 x = x_s[t * vecs + k];
-#pragma unroll
-        for (int r = 0; r < R; ++r) n[r * T + t] = dot16(w[r], x, n[r * T + t]);
+  tc_fence_after();
+  if (!(p.early && warp == 0)) chain_wait();
+  const uint32_t tmem_base = tmem_base_smem;
+  volatile int* abort_p = &abort_flag;
+  const int r0 = (int)((long long)p.V * blockIdx.x / gridDim.x), r1 = (int)((long long)p.V * (blockIdx.x + 1) / gridDim.x);
+  const int tiles = (r1 - r0 + p.rows - 1) / p.rows;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      const uint32_t tok_bar = smem_u32(&bar_tokens);
+      auto load_tokens = [&] {
+        mbar_arrive_expect_tx(tok_bar, (uint32_t)p.k_blocks * N * 128u);
+        for (int kb = 0; kb < p.k_blocks; ++kb) tma_load_2d(tokens + (uint32_t)kb * N * 128u, &tmTokens, tok_bar, kb * 128, 0);
+      };
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      // the tokens once the ring is full, or first
+      const int n_early = p.early ? min(p.stages, p.k_blocks * tiles) : 0;
+      int issued = 0;
+      if (n_early == 0) {
+        chain_wait();
+        load_tokens();
       }
-    }
-    // halving: after the step over lanes `o` apart a lane keeps one half of the sums, the other half is its partner's
-    constexpr int N = R * T;
-    int left = N, first = 0;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      if (left > 1) {
-        const int half = left / 2;
-        const bool up = lane & o;
-#pragma unroll
-        for (int i = 0; i < N / 2; ++i)
-          if (i < half) {
-            const int keep = up ? n[i + half] : n[i], give = up ? n[i] : n[i + half];
-            n[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+      for (int t = 0; t < tiles && ok; ++t) {
+        for (int kb = 0; kb < p.k_blocks; ++kb) {
+          if (!mbar_wait_bounded(smem_u32(&bar_empty[stage]), phase ^ 1u, abort_p)) {
+            latch_status(status, kStatusTimeout, (1 << 28) | (blockIdx.x << 8) | stage);
+            ok = false;
+            break;
           }
-        first += up ? half : 0;
-        left = half;
-      } else {
-        n[0] += __shfl_xor_sync(0xffffffffu, n[0], o);
+          const uint32_t full = smem_u32(&bar_full[stage]);
+          mbar_arrive_expect_tx(full, (uint32_t)p.rows * 128u);
+          tma_load_2d(ring + (uint32_t)stage * kStreamStageBytes, &tmRows, full, kb * 128, r0 + t * p.rows);
+          if (++issued == n_early) {
+            chain_wait();
+            load_tokens();
+          }
+          if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+        }
+      }
+      if (!ok) {
+        // copies already issued land before the block's shared memory goes away
+        for (int s = 0; s < p.stages; ++s) {
+          const uint32_t ph = s < stage ? phase : (phase ^ 1u);
+          for (int it = 0; it < 4096 && !mbar_try_wait(smem_u32(&bar_full[s]), ph); ++it) {}
+        }
+        for (int it = 0; it < 4096 && !mbar_try_wait(tok_bar, 0); ++it) {}
       }
     }
-    const int v = v0 + first / T, t = first % T;
-    constexpr int kCopies = 32 / N;   // lanes that have the same sum
-    if (lane % kCopies == 0 && v < p.V && t < p.T) {
-      const float z = (float)n[0] * p.a_scale[t] * p.b_scale[v];
-      const size_t at = (size_t)t * p.ldC + v;
-      if (p.out == kOutF32) store_one<kOutF32>(p.C, at, z);
-      else if (p.out == kOutF16) store_one<kOutF16>(p.C, at, z);
-      else store_one<kOutBf16>(p.C, at, z);
+  } else if (warp == 1) {
+    if (lane == 0) {
+      constexpr uint32_t idesc = make_idesc_s8(128, N);
+      constexpr uint64_t hi = make_smem_desc_hi(16, 1024);
+      constexpr uint32_t hi32 = uint32_t(hi >> 32), lo_const = uint32_t(hi);
+      const uint32_t ring_lo = (ring & 0x3FFFFu) >> 4, tok_lo = (tokens & 0x3FFFFu) >> 4;
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = tiles == 0 || mbar_wait_bounded(smem_u32(&bar_tokens), 0, abort_p);
+      if (!ok) latch_status(status, kStatusTimeout, (3 << 28) | (blockIdx.x << 8) | 0xff);
+      for (int t = 0; t < tiles && ok; ++t) {
+        const uint32_t a = t & 1u;
+        if (!mbar_wait_bounded(smem_u32(&bar_acc_empty[a]), ((t >> 1) & 1u) ^ 1u, abort_p)) {
+          latch_status(status, kStatusTimeout, (2 << 28) | (blockIdx.x << 8) | a);
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        for (int kb = 0; kb < p.k_blocks; ++kb) {
+          if (!mbar_wait_bounded(smem_u32(&bar_full[stage]), phase, abort_p)) {
+            latch_status(status, kStatusTimeout, (3 << 28) | (blockIdx.x << 8) | stage);
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          const uint32_t w = lo_const | (ring_lo + (uint32_t)stage * (kStreamStageBytes >> 4)), x = lo_const | (tok_lo + (uint32_t)kb * (N * 128 >> 4));
+#pragma unroll
+          for (int k = 0; k < 4; ++k) umma_i8_words<1>(tmem_base + a * N, w + 2 * k, hi32, x + 2 * k, hi32, idesc, (kb > 0 || k > 0) ? 1u : 0u);
+          umma_commit(smem_u32(&bar_empty[stage]));
+          if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+        }
+        if (ok) umma_commit(smem_u32(&bar_acc_full[a]));
+      }
+      umma_commit(smem_u32(&bar_drain));
+      bool drained = false;
+      for (int it = 0; it < (1 << 22) && !drained; ++it) drained = mbar_try_wait(smem_u32(&bar_drain), 0) != 0;
+      if (!drained) latch_status(status, kStatusTimeout, (4 << 28) | (blockIdx.x << 8));
     }
+  } else {
+    const int q = warp & 3, at = q * 32 + lane;   // tensor-memory lanes 32 q and on are this warp's
+    float* scales = a_s[q];
+    for (int t = lane; t < N; t += 32) scales[t] = t < p.T ? p.a_scale[t] : 0.f;
+    __syncwarp();
+    auto row_of = [&](int t) { const int r = r0 + t * p.rows + at; return t < tiles && at < p.rows && r < r1 ? r : -1; };
+    auto scale_of = [&](int r) { return r >= 0 ? __ldg(p.b_scale + r) : 0.f; };
+    // scales of this thread's rows, kAhead tiles early: while the ring streams B such a load takes as long as a tile or two
+    constexpr int kAhead = 4;
+    float b[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) b[u] = scale_of(row_of(u));
+    bool ok = true;
+    for (int t0 = 0; t0 < tiles && ok; t0 += kAhead) {
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int t = t0 + u, r = row_of(t);
+        if (t >= tiles) break;
+        const uint32_t a = u & 1u;
+        if (!mbar_wait_bounded(smem_u32(&bar_acc_full[a]), (t >> 1) & 1u, abort_p)) {
+          latch_status(status, kStatusTimeout, (5 << 28) | (blockIdx.x << 8) | a);
+          ok = false;
+        }
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t taddr = tmem_base + a * N + (uint32_t(q * 32) << 16);
+        size_t out = r >= 0 ? (size_t)r : 0;
+        constexpr int kStep = N < 32 ? 16 : 32;
+#pragma unroll 1
+        for (int c = 0; c < N; c += kStep) {
+          if (c >= p.T) break;
+          uint32_t x[kStep];
+          if constexpr (kStep == 16) tmem_ld_32x16(taddr + c, x);
+          else tmem_ld_32x32(taddr + c, x);
+          tmem_ld_wait();
+          if (r >= 0) {
+#pragma unroll
+            for (int i = 0; i < kStep; ++i)
+              if (c + i < p.T) store_one<OUT>(p.C, out + (size_t)(c + i) * p.ldC, (float)(int)x[i] * scales[c + i] * b[u]);
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&bar_acc_empty[a]));
+        b[u] = scale_of(row_of(t + kAhead));
+      }
+    }
+  }
+  chain_release();
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    __syncwarp();
+    tc_fence_after();
+    tmem_dealloc(tmem_base, kCols);
   }
 }
 

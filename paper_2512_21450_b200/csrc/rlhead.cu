@@ -415,11 +415,16 @@ cudaError_t set_smem_attr_int8() {
   also(set_smem_attr<EpiScale<kOutBf16, false, 4>, 0, 0>());
   also(set_smem_attr<EpiScale<kOutF32, false, 4>, 0, 0>());
   also(set_smem_attr<EpiScale<kOutF16, false, 4>, 0, 0>());
-  auto few = [&](auto kernel) { also(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewSmem)); };
-  few(int8_few_kernel<1, 8>);
-  few(int8_few_kernel<2, 8>);
-  few(int8_few_kernel<4, 4>);
-  few(int8_few_kernel<8, 4>);
+  auto stream = [&](auto kernel) { also(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kStreamSmem)); };
+  auto stream_out = [&](auto n) {
+    constexpr int N = decltype(n)::value;
+    stream(int8_stream_kernel<N, kOutBf16>);
+    stream(int8_stream_kernel<N, kOutF32>);
+    stream(int8_stream_kernel<N, kOutF16>);
+  };
+  stream_out(std::integral_constant<int, 16>());
+  stream_out(std::integral_constant<int, 32>());
+  stream_out(std::integral_constant<int, 64>());
   return e;
 }
 
@@ -1866,8 +1871,9 @@ static rl_status check_int8(const void* B, int64_t ldB, const float* b_scale, in
   return RL_OK;
 }
 
-rl_status rl_int8_matmul(rl_ctx* c, const int8_t* A, int64_t ldA, const float* a_scale, const int8_t* B, int64_t ldB, const float* b_scale,
-                         int64_t T, int64_t d, int64_t V, void* C, int c_dtype, int64_t ldC) {
+// early: see StreamParams.
+static rl_status int8_matmul(rl_ctx* c, const int8_t* A, int64_t ldA, const float* a_scale, const int8_t* B, int64_t ldB,
+                             const float* b_scale, int64_t T, int64_t d, int64_t V, void* C, int c_dtype, int64_t ldC, int early) {
   if (!c) return RL_ERR_INVALID_ARG;
   rl_status s = check_int8(B, ldB, b_scale, T, d, V, C, c_dtype, ldC);
   if (s != RL_OK) return s;
@@ -1876,19 +1882,25 @@ rl_status rl_int8_matmul(rl_ctx* c, const int8_t* A, int64_t ldA, const float* a
   if (ldA < d) return RL_ERR_SHAPE;
   if ((reinterpret_cast<uintptr_t>(A) & 15) || ldA % 16 || (reinterpret_cast<uintptr_t>(a_scale) & 3)) return RL_ERR_ALIGNMENT;
   const OnDevice on(c);
-  const int64_t few = T <= 1 ? 1 : T <= 2 ? 2 : T <= 4 ? 4 : kFewTokens, few_bytes = few * ((d + 15) / 16 * 16);
-  if (T <= kFewTokens && few_bytes <= kFewSmem) {
-    const FewParams p = {A, a_scale, B, b_scale, ldA, ldB, ldC, (int)T, (int)d, (int)V, c_dtype, C};
+  const int k_blocks = (int)((d + 127) / 128), n_stream = T <= 16 ? 16 : T <= 32 ? 32 : 64;
+  if (T <= 64 && stream_stages(n_stream, k_blocks) >= kStreamMinStages) {
+    StreamParams p = {a_scale, b_scale, (int)T, (int)V, k_blocks, 0, stream_stages(n_stream, k_blocks), early, C, ldC};
+    const int64_t per = (V + c->grid[1] - 1) / c->grid[1], tiles = (per + 127) / 128;
+    p.rows = (int)((per + tiles - 1) / tiles);
+    const int blocks = (int)(V < c->grid[1] ? V : c->grid[1]);
+    CUtensorMap x, w;
+    if (!map_kmajor_i8(c, &x, A, (uint64_t)T, (uint64_t)d, (uint64_t)ldA, (uint32_t)n_stream) ||
+        !map_kmajor_i8(c, &w, B, (uint64_t)V, (uint64_t)d, (uint64_t)ldB, (uint32_t)p.rows))
+      return RL_ERR_CUDA;
     const int pr = prof_begin(c, 0);
-    auto stream = [&](auto kernel, int rows) {
-      int64_t blocks = (V + 16 * rows - 1) / (16 * rows);   // sixteen warps
-      if (blocks > (int64_t)c->n_sm * 2) blocks = (int64_t)c->n_sm * 2;
-      launch_smem(c, kernel, (int)blocks, 512, (size_t)few_bytes, p);
+    auto go = [&](auto n) {
+      constexpr int N = decltype(n)::value;
+      auto kernel = c_dtype == RL_FP32 ? int8_stream_kernel<N, kOutF32> : c_dtype == RL_FP16 ? int8_stream_kernel<N, kOutF16> : int8_stream_kernel<N, kOutBf16>;
+      launch_smem(c, kernel, blocks, kStreamThreads, kStreamSmem, x, w, p, c->dstatus);
     };
-    if (few == 1) stream(int8_few_kernel<1, 8>, 8);
-    else if (few == 2) stream(int8_few_kernel<2, 8>, 8);
-    else if (few == 4) stream(int8_few_kernel<4, 4>, 4);
-    else stream(int8_few_kernel<kFewTokens, 4>, 4);
+    if (n_stream == 16) go(std::integral_constant<int, 16>());
+    else if (n_stream == 32) go(std::integral_constant<int, 32>());
+    else go(std::integral_constant<int, 64>());
     prof_end(c, pr, 0);
     c->launches++;
     return cuda_ok();
@@ -1908,6 +1920,11 @@ rl_status rl_int8_matmul(rl_ctx* c, const int8_t* A, int64_t ldA, const float* a
   const ScaleParams p = {a_scale, b_scale, (int)V, C, ldC};
   return c_dtype == RL_FP32 ? int8_tiles<kOutF32>(c, a, b, cg, sh, p, T)
          : c_dtype == RL_FP16 ? int8_tiles<kOutF16>(c, a, b, cg, sh, p, T) : int8_tiles<kOutBf16>(c, a, b, cg, sh, p, T);
+}
+
+rl_status rl_int8_matmul(rl_ctx* c, const int8_t* A, int64_t ldA, const float* a_scale, const int8_t* B, int64_t ldB, const float* b_scale,
+                         int64_t T, int64_t d, int64_t V, void* C, int c_dtype, int64_t ldC) {
+  return int8_matmul(c, A, ldA, a_scale, B, ldB, b_scale, T, d, V, C, c_dtype, ldC, 0);
 }
 
 // Quantised rows of int8_linear in the workspace, their scales behind them.
@@ -1931,7 +1948,7 @@ rl_status rl_int8_linear(rl_ctx* c, const void* X, int x_dtype, int64_t ldX, con
   float* a_scale = T > 0 ? reinterpret_cast<float*>(static_cast<char*>(c->ws) + int8_rows_bytes(T, d)) : nullptr;
   const int64_t ldA = (int64_t)align_up((size_t)d, 16);
   if ((s = rl_quantize_rows(c, X, x_dtype, ldX, T, d, A, ldA, a_scale)) != RL_OK || T == 0) return s;
-  return rl_int8_matmul(c, A, ldA, a_scale, B, ldB, b_scale, T, d, V, C, c_dtype, ldC);
+  return int8_matmul(c, A, ldA, a_scale, B, ldB, b_scale, T, d, V, C, c_dtype, ldC, 1);
 }
 
 rl_status rl_token_logprobs_int8(rl_ctx* c, const void* H, int64_t ldH, const int8_t* W, int64_t ldW, const float* w_scale,
