@@ -219,7 +219,8 @@ def _load_host_calls(lib):
         return
     host.bind(*(ctypes.cast(getattr(lib, name), c_void_p).value for name in (
         "rl_workspace_bytes", "rl_workspace_bytes_logprobs", "rl_set_workspace", "rl_grpo_advantages_ex", "rl_kl_shaped_returns",
-        "rl_token_loss", "rl_token_logprobs", "rl_policy_loss_fwd_bwd_ex")))
+        "rl_token_loss", "rl_token_logprobs", "rl_policy_loss_fwd_bwd_ex", "rl_workspace_bytes_ce", "rl_cross_entropy_fwd_bwd",
+        "rl_quantize_rows", "rl_workspace_bytes_int8_linear", "rl_int8_linear", "rl_token_logprobs_int8")))
     _host = host
 
 
@@ -503,6 +504,16 @@ class Context:
         token_loss [T], metrics [8]); a gradient that is not wanted is not formed and left out.  H [T, d] is bf16, or int8 with H_scale
         [T] (rl_quantize_rows); dH is the gradient of what that stands for."""
         self._bind_stream()
+        if self._ws is not None and loss is None and dH is None and dW is None and not accumulate_dW:
+            got = _host.cross_entropy(self._address, self.device.index, self._ws, H, W, targets, mask, label_smoothing, z_coef, token_weight,
+                                      token_count, H_scale, want_dH, want_dW, dW_bf16, dH_fp32)
+            if _handled(got, "rl_cross_entropy_fwd_bwd"):
+                out = dict(loss=got[0], logp=got[1], lse=got[2], token_loss=got[3], metrics=got[4])
+                if want_dH:
+                    out["dH"] = got[5]
+                if want_dW:
+                    out["dW"] = got[-1]
+                return out
         T, d = H.shape
         V = W.shape[0]
         assert W.dtype == torch.bfloat16 and W.dim() == 2 and W.shape[1] == d and W.stride(1) == 1
@@ -551,6 +562,10 @@ class Context:
     def rl_quantize_rows(self, X, Q=None, scale=None):
         """Rows of X [N, d] (bf16, fp16 or fp32) in 8 bits: (Q [N, d] int8 whose rows start on multiples of 16 bytes, scale [N] fp32)."""
         self._bind_stream()
+        if Q is None and scale is None:
+            out = _host.quantize_rows(self._address, self.device.index, X)
+            if _handled(out, "rl_quantize_rows"):
+                return out
         N, d = X.shape
         if Q is None:
             Q = torch.empty(N, (d + 15) // 16 * 16, dtype=torch.int8, device=X.device)[:, :d]
@@ -587,6 +602,10 @@ class Context:
     def rl_int8_linear(self, X, Wq, w_scale, out_dtype=torch.bfloat16, out=None):
         """Logits [T, V] of hidden states X [T, d] (bf16, fp16 or fp32) under a head held in 8 bits: Wq [V, d] int8, w_scale [V]."""
         self._bind_stream()
+        if self._ws is not None and out is None and out_dtype in DTYPES:
+            got = _host.int8_linear(self._address, self.device.index, self._ws, X, Wq, w_scale, DTYPES[out_dtype])
+            if _handled(got, "rl_int8_linear"):
+                return got[0]
         T, d = X.shape
         assert Wq.shape[1] == d
         out = self._int8_out(T, Wq, w_scale, out_dtype, out)
@@ -601,6 +620,10 @@ class Context:
     def rl_token_logprobs_int8(self, H, Wq, w_scale, tokens, mask=None):
         """rl_token_logprobs under a head held in 8 bits: (logp, entropy, lse), each [T]."""
         self._bind_stream()
+        if self._ws is not None:
+            out = _host.token_logprobs_int8(self._address, self.device.index, self._ws, H, Wq, w_scale, tokens, mask)
+            if _handled(out, "rl_token_logprobs_int8"):
+                return out
         T, d = H.shape
         V = Wq.shape[0]
         assert H.dtype == torch.bfloat16 and Wq.dtype == torch.int8 and Wq.shape[1] == d

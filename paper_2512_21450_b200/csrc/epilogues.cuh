@@ -267,9 +267,9 @@ struct GradParams {
   const float* ce;
   int V;
   int vocab_base;  // global column of the slab's column 0
-  float uniform;   // cross entropy: e / ((1 - e) V) of labels smoothed by e
+  float uniform;   // cross entropy: e / ((1 - e) V) of labels smoothed by e, what a column gets of the target's coefficient
 };
-// CE: the gradient of the cross entropy, g_tj = cp_t p_tj - ct_t (1[j = y_t] + uniform), ct_t = w_t (1 - e) in place of ce_t.
+// CE: the gradient of the cross entropy, g_tj = cp_t p_tj - ct_t (1[j = y_t] + uniform), ct_t in place of ce_t (combine_loss_kernel).
 template <int W, bool CE = false>
 struct EpiGrad {
   static constexpr bool kParts = false;
@@ -389,6 +389,7 @@ struct AccParams {
   int slab_cap, slab_one, slab_index;
   int row_base;
   int slice_add;   // stream-K launches: output slices past the first are always added to
+  const float* scale;   // kAccScaled, kAccHalf: what every element is multiplied with
   int tile_cols;   // > 0: k_slice > 0 names slot k_slice - 1, a box of tile_cols columns x tile_rows rows of its own
   int tile_rows;
 };
@@ -397,9 +398,11 @@ struct AccParams {
 // DRAM one box at a time.  dW of 151936 words, d = 2048, four warps / eight: stores 282 / 264 us at 100 rows, 380 / 340 at 300, 468 / 430 at
 // 512, and slower from 1000 rows on; adds 542 / 425, 587 / 446, 602 / 524 (the four without prefetches; with them 413 / 494 / 544; a
 // plain kernel that adds in this order takes 400).
-// HALF: stored as bf16 instead, through a map of 64-column boxes (never added to, tiles not cut).
-template <int W, bool HALF = false>
+// OUT: as it is; times a number; or times a number and stored as bf16, through a map of 64-column boxes (never added to).
+enum AccOut { kAccPlain = 0, kAccScaled = 1, kAccHalf = 2 };
+template <int W, int OUT = kAccPlain>
 struct EpiAccW {
+  static constexpr bool HALF = OUT == kAccHalf;
   static constexpr bool kParts = !HALF;
   static constexpr int kSideWarps = 0;
   static constexpr bool kFeeds = false, kAhead = W == 8 && !HALF, kInt8 = false;
@@ -410,6 +413,7 @@ struct EpiAccW {
   struct State {
     int k_slice;
     int add;
+    float scale;
     uint32_t n_issued;   // chunks handed to the TMA unit so far (selects the staging buffer)
     int next_row, next_col;   // this warp's part of the next tile (row -1: none)
   };
@@ -420,15 +424,19 @@ struct EpiAccW {
   }
   __device__ static __forceinline__ void begin_unit(const Params& p, State& st, int, int, int, int, int, int k_slice) {
     st.k_slice = k_slice;
+    if (OUT != kAccPlain) st.scale = *p.scale;
     st.add = p.accumulate == 2 ? p.slab_index + 1 < slab_count(*p.n_valid, p.slab_cap, p.slab_one) : p.accumulate;
   }
   __device__ static __forceinline__ void chunk(const Params& p, State& st, int m_tile, int n_tile, int c,
-                                               int row_in_tile, int m_rows, const float (&v)[32],
+                                               int row_in_tile, int m_rows, const float (&acc)[32],
                                                const CUtensorMap* tmC, uint32_t staging) {
     const int lane = threadIdx.x & 31;
     const int row0 = m_tile * BM + (row_in_tile - lane);   // first row of this warp's 32
     const int col0 = n_tile * BN + c * 32;
     if (row0 >= m_rows || col0 >= p.n_cols) return;        // warp-uniform
+    float v[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = OUT == kAccPlain ? acc[i] : acc[i] * st.scale;
     if constexpr (HALF) {
       uint32_t w[16];
 #pragma unroll

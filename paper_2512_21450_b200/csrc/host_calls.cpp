@@ -21,6 +21,12 @@ struct Abi {
   decltype(&rl_token_loss) token_loss;
   decltype(&rl_token_logprobs) token_logprobs;
   decltype(&rl_policy_loss_fwd_bwd_ex) policy_loss_fwd_bwd_ex;
+  decltype(&rl_workspace_bytes_ce) workspace_bytes_ce;
+  decltype(&rl_cross_entropy_fwd_bwd) cross_entropy_fwd_bwd;
+  decltype(&rl_quantize_rows) quantize_rows;
+  decltype(&rl_workspace_bytes_int8_linear) workspace_bytes_int8_linear;
+  decltype(&rl_int8_linear) int8_linear;
+  decltype(&rl_token_logprobs_int8) token_logprobs_int8;
 } abi;
 
 // Thrown where the general path has to take over.
@@ -30,6 +36,7 @@ struct General {};
 struct Args {
   PyObject* const* a;
   Py_ssize_t n, i = 0;
+  int device = -1;   // >= 0: every tensor read from then on lies there
   Args(PyObject* const* args, Py_ssize_t nargs, Py_ssize_t expect) : a(args), n(nargs) {
     if (n != expect) throw General();
   }
@@ -65,7 +72,7 @@ struct Args {
     }
     if (!THPVariable_CheckExact(o)) throw General();
     const at::Tensor& t = THPVariable_Unpack(o);
-    if (!t.defined() || !t.is_cuda() || !t.has_storage()) throw General();
+    if (!t.defined() || !t.is_cuda() || !t.has_storage() || (device >= 0 && t.get_device() != device)) throw General();
     return &t;
   }
   const at::Tensor* of(at::ScalarType type, bool none_ok) {
@@ -87,8 +94,8 @@ struct Args {
     return t;
   }
   // rows of bf16, contiguous within a row
-  const at::Tensor* rows() {
-    const at::Tensor* t = of(at::kBFloat16, false);
+  const at::Tensor* rows(at::ScalarType type = at::kBFloat16) { return matrix(of(type, false)); }
+  const at::Tensor* matrix(const at::Tensor* t) {
     if (t->dim() != 2 || t->stride(1) != 1) throw General();
     return t;
   }
@@ -106,7 +113,7 @@ struct Unlocked {
 
 // What a call returns.
 struct Outputs {
-  at::Tensor t[4];
+  at::Tensor t[8];
   int n = 0;
   void* add(at::Tensor x) {
     t[n] = std::move(x);
@@ -291,6 +298,134 @@ PyObject* policy_loss(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   });
 }
 
+// Row stride of a matrix; of a single row its length (8-bit rows: the next multiple of 16).
+int64_t row_stride(const at::Tensor* t, int64_t unit = 1) {
+  return t->size(0) > 1 ? t->stride(0) : (t->size(1) + unit - 1) / unit * unit;
+}
+const at::ScalarType kTypes[] = {at::kBFloat16, at::kFloat, at::kHalf};   // rl_dtype
+int dtype_of(const at::Tensor* t) {
+  for (int i = 0; i < 3; ++i)
+    if (t->scalar_type() == kTypes[i]) return i;
+  throw General();
+}
+void room(rl_ctx* c, const at::Tensor* ws, rl_status asked, size_t need) {
+  if (asked != RL_OK || !ws || (size_t)ws->numel() < need) throw General();
+  if (abi.set_workspace(c, ws->data_ptr(), (size_t)ws->numel()) != RL_OK) throw General();
+}
+
+// (context, device, workspace, H, W, targets, mask, label_smoothing, z_coef, token_weight, token_count, H_scale, want_dH, want_dW, dW_bf16,
+//  dH_fp32) -> (loss, logp, lse, token_loss, metrics, dH where wanted, dW where wanted)
+PyObject* cross_entropy(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  return guarded([&](Outputs& out) {
+    Args a(args, nargs, 16);
+    rl_ctx* c = a.context();
+    a.device = a.small();
+    const at::Tensor *ws = a.tensor(false), *H = a.matrix(a.tensor(false)), *W = a.rows();
+    const int64_t T = H->size(0), d = H->size(1), V = W->size(0);
+    if (T == 0 || W->size(1) != d) throw General();
+    const at::Tensor *targets = a.array(at::kInt, T, false), *mask = a.mask(T);
+    rl_ce_opts o;
+    memset(&o, 0, sizeof(o));
+    o.struct_size = sizeof(o);
+    o.label_smoothing = a.real();
+    o.z_coef = a.real();
+    o.token_weight = data<float>(a.values(T, true));
+    o.token_count = data<int64_t>(a.array(at::kLong, 1, true));
+    const at::Tensor* scale = a.values(T, true);
+    o.H_scale = data<float>(scale);
+    if (H->scalar_type() != (scale ? at::kChar : at::kBFloat16)) throw General();
+    const bool want_dH = a.integer() != 0, want_dW = a.integer() != 0;
+    o.dW_dtype = a.integer() != 0 ? RL_BF16 : RL_FP32;
+    o.dH_dtype = a.integer() != 0 ? RL_FP32 : RL_BF16;
+    size_t need = 0;
+    const rl_status asked = want_dH || want_dW ? abi.workspace_bytes_ce(c, T, d, V, want_dW ? o.dW_dtype : RL_FP32, &need)
+                                               : abi.workspace_bytes_logprobs(c, T, d, V, &need);
+    room(c, ws, asked, need);
+    const void *ph = H->data_ptr(), *pw = W->data_ptr();
+    const int64_t ldH = row_stride(H, scale ? 16 : 1), ldW = row_stride(W);
+    const int32_t* pt = data<int32_t>(targets);
+    const uint8_t* pm = static_cast<const uint8_t*>(data<void>(mask));
+    const auto options = W->options().requires_grad(false);
+    Unlocked u;
+    float* loss = out.values(1, *W);
+    o.logp_out = out.values(T, *W);
+    o.lse_out = out.values(T, *W);
+    o.token_loss_out = out.values(T, *W);
+    o.metrics_out = out.values(8, *W);
+    void* dH = want_dH ? out.add(at::empty({T, d}, options.dtype(kTypes[o.dH_dtype]))) : nullptr;
+    void* dW = want_dW ? out.add(at::empty({V, d}, options.dtype(kTypes[o.dW_dtype]))) : nullptr;
+    return abi.cross_entropy_fwd_bwd(c, ph, ldH, pw, ldW, pt, pm, T, d, V, loss, dH, dW, &o);
+  });
+}
+
+// (context, device, X) -> (rows of 8-bit integers, scale)
+PyObject* quantize_rows(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  return guarded([&](Outputs& out) {
+    Args a(args, nargs, 3);
+    rl_ctx* c = a.context();
+    a.device = a.small();
+    const at::Tensor* X = a.matrix(a.tensor(false));
+    const int64_t n = X->size(0), d = X->size(1), ld = (d + 15) / 16 * 16, ldX = row_stride(X);
+    if (n == 0 || d == 0) throw General();
+    const int type = dtype_of(X);
+    const void* px = X->data_ptr();
+    Unlocked u;
+    at::Tensor q = at::empty({n, ld}, X->options().dtype(at::kChar).requires_grad(false));
+    int8_t* pq = static_cast<int8_t*>(q.data_ptr());
+    out.add(ld == d ? q : q.narrow(1, 0, d));
+    float* scale = out.values(n, *X);
+    return abi.quantize_rows(c, px, type, ldX, n, d, pq, ld, scale);
+  });
+}
+
+// (context, device, workspace, X, Wq, w_scale, out_dtype) -> (logits,)
+PyObject* int8_linear(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  return guarded([&](Outputs& out) {
+    Args a(args, nargs, 7);
+    rl_ctx* c = a.context();
+    a.device = a.small();
+    const at::Tensor *ws = a.tensor(false), *X = a.matrix(a.tensor(false)), *W = a.rows(at::kChar);
+    const int64_t T = X->size(0), d = X->size(1), V = W->size(0);
+    if (T == 0 || W->size(1) != d) throw General();
+    const at::Tensor* scale = a.values(V, false);
+    const int type = dtype_of(X), out_type = a.small();
+    if (out_type < 0 || out_type > 2) throw General();
+    size_t need = 0;
+    const rl_status asked = abi.workspace_bytes_int8_linear(c, T, d, &need);
+    room(c, ws, asked, need);
+    const void* px = X->data_ptr();
+    const int8_t* pw = data<int8_t>(W);
+    const float* ps = data<float>(scale);
+    const int64_t ldX = row_stride(X), ldW = row_stride(W, 16);
+    Unlocked u;
+    void* C = out.add(at::empty({T, V}, X->options().dtype(kTypes[out_type]).requires_grad(false)));
+    return abi.int8_linear(c, px, type, ldX, pw, ldW, ps, T, d, V, C, out_type, V);
+  });
+}
+
+// (context, device, workspace, H, Wq, w_scale, tokens, mask) -> (logp, entropy, lse)
+PyObject* token_logprobs_int8(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  return guarded([&](Outputs& out) {
+    Args a(args, nargs, 8);
+    rl_ctx* c = a.context();
+    a.device = a.small();
+    const at::Tensor *ws = a.tensor(false), *H = a.rows(), *W = a.rows(at::kChar);
+    const int64_t T = H->size(0), d = H->size(1), V = W->size(0);
+    if (T == 0 || W->size(1) != d) throw General();
+    const at::Tensor *scale = a.values(V, false), *tokens = a.array(at::kInt, T, false), *mask = a.mask(T);
+    bind_workspace(c, ws, abi.workspace_bytes_logprobs, T, d, V);
+    const void* ph = H->data_ptr();
+    const int8_t* pw = data<int8_t>(W);
+    const float* ps = data<float>(scale);
+    const int64_t ldH = row_stride(H), ldW = row_stride(W, 16);
+    const int32_t* pt = data<int32_t>(tokens);
+    const uint8_t* pm = static_cast<const uint8_t*>(data<void>(mask));
+    Unlocked u;
+    float *logp = out.values(T, *H), *ent = out.values(T, *H), *lse = out.values(T, *H);
+    return abi.token_logprobs_int8(c, ph, ldH, pw, ldW, ps, pt, pm, T, d, V, logp, ent, lse);
+  });
+}
+
 // (addresses of the ABI's functions, in the order of Abi)
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   void** slot = reinterpret_cast<void**>(&abi);
@@ -315,6 +450,10 @@ PyMethodDef methods[] = {
     {"token_loss", reinterpret_cast<PyCFunction>(token_loss), METH_FASTCALL, nullptr},
     {"token_logprobs", reinterpret_cast<PyCFunction>(token_logprobs), METH_FASTCALL, nullptr},
     {"policy_loss", reinterpret_cast<PyCFunction>(policy_loss), METH_FASTCALL, nullptr},
+    {"cross_entropy", reinterpret_cast<PyCFunction>(cross_entropy), METH_FASTCALL, nullptr},
+    {"quantize_rows", reinterpret_cast<PyCFunction>(quantize_rows), METH_FASTCALL, nullptr},
+    {"int8_linear", reinterpret_cast<PyCFunction>(int8_linear), METH_FASTCALL, nullptr},
+    {"token_logprobs_int8", reinterpret_cast<PyCFunction>(token_logprobs_int8), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

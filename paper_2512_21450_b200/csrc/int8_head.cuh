@@ -185,6 +185,13 @@ struct ColumnScales {
   }
 };
 
+// Eight epilogue warps in place of four up to these widths: the products take half the time that bf16's do, so the epilogue shows to
+// twice the width, less where it has a box to wait for.  8192 rows x 151936 words, four / eight, d = 512 / 1024 / 1536 / 2048 / 2560:
+// statistics 1209 / 1454 / 1728 / 1900 / 2155 us, 953 / 1207 / 1456 / 1846 / 2255; bf16 logits 972 / 1277 / 1591 / 1910 / 2283 us, 856 / 1262 /
+// 1682 / 2114 / 2486; fp32 logits 1211 / 1637 / 2113 / 2408 / 2835, 1080 / 1619 / 2087 / 2527 / 2966.
+constexpr int kEightWarpsStatsI8 = 2048;
+constexpr int kEightWarpsScale = 768;
+
 // Statistics of RowStats over those logits: scoring under a head held in 8 bits.
 struct Int8StatsParams : RowStats::Params {
   const float* row_scale;   // compact rows

@@ -87,6 +87,7 @@ constexpr int kWideGain = 96;              // time of a 256 x 512 tile, in % of 
 constexpr int kMergeBlocks = 512;          // blocks per merge launch when a call makes several (kLossThreads threads each)
 constexpr size_t kTicketOffset = 192;      // in the device block: blocks that are done, of the loss kernels of a step (cleared by
                                            // its row preparation) and of rl_token_loss (one launch: 0 whenever none runs)
+constexpr size_t kScaleOffset = 128;       // in the device block: what the gradients of a cross entropy are multiplied with
 constexpr int kDhSplitMax = 4;             // most K slices (separate fp32 accumulators) of the dH pass
 constexpr int kSlabColsMax = 148 * 256;    // vocabulary columns of one gradient slab (148 tiles of 256: two per SM pair)
 
@@ -409,6 +410,9 @@ cudaError_t set_smem_attr_int8() {
   cudaError_t e = set_smem_attr<EpiStatsI8<4>, 0, 0>();
   auto also = [&](cudaError_t x) { if (e == cudaSuccess) e = x; };
   also(set_smem_attr<EpiStatsI8<8>, 0, 0>());
+  also(set_smem_attr<EpiScale<kOutBf16, true, 8>, 0, 0>());
+  also(set_smem_attr<EpiScale<kOutF32, true, 8>, 0, 0>());
+  also(set_smem_attr<EpiScale<kOutF16, true, 8>, 0, 0>());
   also(set_smem_attr<EpiScale<kOutBf16, true, 4>, 0, 0>());
   also(set_smem_attr<EpiScale<kOutF32, true, 4>, 0, 0>());
   also(set_smem_attr<EpiScale<kOutF16, true, 4>, 0, 0>());
@@ -557,7 +561,8 @@ rl_status int8_tiles(rl_ctx* c, const CUtensorMap& a, const CUtensorMap& b, int 
   const bool ok = OUT == kOutF32 ? map_out_f32(c, &out, static_cast<float*>(p.C), (uint64_t)T, (uint64_t)p.V, (uint64_t)p.ldC, 1, (uint64_t)T)
                                  : map_out_bf16(c, &out, p.C, (uint64_t)T, (uint64_t)p.V, (uint64_t)p.ldC);
   if (!ok) return RL_ERR_CUDA;
-  launch_gemm<EpiScale<OUT, true, 4>, 0, 0>(c, cg, 0, a, b, out, out, sh, p);
+  if (sh.k_cap * 2 <= kEightWarpsScale) launch_gemm<EpiScale<OUT, true, 8>, 0, 0>(c, cg, 0, a, b, out, out, sh, p);
+  else                                  launch_gemm<EpiScale<OUT, true, 4>, 0, 0>(c, cg, 0, a, b, out, out, sh, p);
   return cuda_ok();
 }
 
@@ -737,19 +742,19 @@ rl_status run_forward(rl_ctx* c, const WsLayout& L, const void* H, int64_t ldH, 
   ep.partials = reinterpret_cast<float4*>(ws + L.partials);
   ep.part_stride = L.Tpad;
   ep.V = (int)V;
-  auto stats = [&](auto four, auto eight, const auto& params, int64_t k) {
-    if (k <= kEightWarpsMaxK) launch_gemm<decltype(eight), 0, 0>(c, cg, 0, tmA, tmB, tmA, tmA, sh, params);
-    else                      launch_gemm<decltype(four), 0, 0>(c, cg, 0, tmA, tmB, tmA, tmA, sh, params);   // no output map
+  auto stats = [&](auto four, auto eight, const auto& params, bool narrow) {
+    if (narrow) launch_gemm<decltype(eight), 0, 0>(c, cg, 0, tmA, tmB, tmA, tmA, sh, params);
+    else        launch_gemm<decltype(four), 0, 0>(c, cg, 0, tmA, tmB, tmA, tmA, sh, params);   // no output map
   };
   if (plan.W_scale) {
     Int8StatsParams ei;
     static_cast<RowStats::Params&>(ei) = ep;
     ei.row_scale = pp.scale_c;
     ei.col_scale = plan.W_scale;
-    stats(EpiStatsI8<4>(), EpiStatsI8<8>(), ei, int8_k(d));
+    stats(EpiStatsI8<4>(), EpiStatsI8<8>(), ei, d <= kEightWarpsStatsI8);
   } else if (plan.sums) {
     RowStatsOf<true>::Params es = {ep.tokens_c, ep.partials, ep.part_stride, ep.V};
-    stats(EpiStats<4, true>(), EpiStats<8, true>(), es, d);
+    stats(EpiStats<4, true>(), EpiStats<8, true>(), es, d <= kEightWarpsMaxK);
   } else if (!kl) {
     if (d <= kEightWarpsMaxK) launch_gemm<EpiStats<8>, 0, 0>(c, cg, 0, tmA, tmB, tmA, tmA, sh, ep);
     else                      launch_gemm<EpiStats<4>, 0, 0>(c, cg, 0, tmA, tmB, tmA, tmA, sh, ep);   // no output map
@@ -847,8 +852,9 @@ rl_status rl_create(rl_ctx** out, int device) {
             set_smem_attr<EpiSweepOf<true>, 0, 0>() == cudaSuccess && set_smem_attr<EpiGrad<4, true>, 0, 0>() == cudaSuccess &&
             set_smem_attr<EpiGrad<8, true>, 0, 0>() == cudaSuccess && set_smem_attr<EpiAccFedOf<kGradCE>, 0, 1>() == cudaSuccess &&
             set_smem_attr_one<EpiAccFedOf<kGradCE>, 0, 1, 2, kTileWide>() == cudaSuccess &&
-            set_smem_attr<EpiAccW<4, true>, 1, 1>() == cudaSuccess && set_smem_attr<EpiAccScatter<4, true>, 1, 1>() == cudaSuccess &&
-            set_smem_attr<EpiAccScatter<8, true>, 1, 1>() == cudaSuccess && set_smem_attr_int8() == cudaSuccess;
+            set_smem_attr<EpiAccW<4, kAccHalf>, 1, 1>() == cudaSuccess && set_smem_attr<EpiAccScatter<4, kAccHalf>, 1, 1>() == cudaSuccess &&
+            set_smem_attr<EpiAccScatter<8, kAccHalf>, 1, 1>() == cudaSuccess && set_smem_attr<EpiAccW<4, kAccScaled>, 1, 1>() == cudaSuccess &&
+            set_smem_attr<EpiAccScatter<4, kAccScaled>, 1, 1>() == cudaSuccess && set_smem_attr<EpiAccScatter<8, kAccScaled>, 1, 1>() == cudaSuccess && set_smem_attr_int8() == cudaSuccess;
   if (!ok) { cudaFree(c->dstatus); delete c; return RL_ERR_CUDA; }
   {
     // how many CTA pairs can be resident at once (pairs must share a TPC): the persistent grid
@@ -1406,6 +1412,7 @@ static rl_status loss_fwd_bwd_impl(rl_ctx* c, const void* H, int64_t ldH, const 
     p.smooth = ce->smooth;
     p.z_coef = ce->z_coef;
     p.V = (int)V;
+    p.out_scale = reinterpret_cast<float*>(reinterpret_cast<char*>(c->dstatus) + kScaleOffset);
     p.lse_out = ce->lse_out;
     p.each_out = ce->each_out;
   }
@@ -1551,6 +1558,7 @@ static rl_status loss_fwd_bwd_impl(rl_ctx* c, const void* H, int64_t ldH, const 
     src.row_map = row_map;
     src.dH = dH;
     src.f32 = o.dH_dtype;
+    src.scale = p.out_scale;
     const int rows_cap = L.Ts;   // the valid rows are cut into equal slabs of at most Ts rows on the device
     // stream-K parts that finish a tile are added to the second accumulator buffer: it starts at zero
     if (dh_uses_stream_k(c)) cudaMemsetAsync(dH_acc + (size_t)L.Ts * d, 0, (size_t)L.Ts * d * 4, st);
@@ -1740,6 +1748,7 @@ static rl_status loss_fwd_bwd_impl(rl_ctx* c, const void* H, int64_t ldH, const 
         ep.n_cols = (int)d; ep.accumulate = o.accumulate_dW ? 1 : reverse ? 2 : (r > 0 ? 1 : 0);
         ep.n_valid = n_valid; ep.slab_cap = L.Tc; ep.slab_one = L.Ts; ep.slab_index = r;
         ep.row_base = vocab_base + c0; ep.slice_add = 0; ep.tile_cols = 0;
+        ep.scale = p.out_scale;
         if (dH_beside && !report && cs == n_col_slabs - 1) {
           src.shape = dh_shape;
           auto dW_and_dH = [&](auto epi) {
@@ -1751,13 +1760,15 @@ static rl_status loss_fwd_bwd_impl(rl_ctx* c, const void* H, int64_t ldH, const 
           // (a worker with one or two tiles has nothing for more epilogue warps to overlap: the smallest step 52.2 -> 52.9 us)
           const long long tiles = (long long)d_tiles * ((cols + BN - 1) / BN);
           const bool eight = T <= kFewRows && tiles >= 4 * dh_workers;
-          if (half_dW)    eight ? dW_and_dH(EpiAccScatter<8, true>()) : dW_and_dH(EpiAccScatter<4, true>());
-          else if (eight) dW_and_dH(EpiAccScatter<8>());
-          else            dW_and_dH(EpiAccScatter<4>());
-        } else if (half_dW) {
-          launch_gemm<EpiAccW<4, true>, 1, 1>(c, c->cta_group, 3, tmG_mn, tmHc_mn, tm_dW, tm_dW, sh, ep);
+          auto by_warps = [&](auto four, auto more) { eight ? dW_and_dH(more) : dW_and_dH(four); };
+          if (!ce)          by_warps(EpiAccScatter<4>(), EpiAccScatter<8>());
+          else if (half_dW) by_warps(EpiAccScatter<4, kAccHalf>(), EpiAccScatter<8, kAccHalf>());
+          else              by_warps(EpiAccScatter<4, kAccScaled>(), EpiAccScatter<8, kAccScaled>());
         } else {
-          launch_gemm<EpiAcc, 1, 1>(c, c->cta_group, 3, tmG_mn, tmHc_mn, tm_dW, tm_dW, sh, ep);
+          auto dW_alone = [&](auto epi) { launch_gemm<decltype(epi), 1, 1>(c, c->cta_group, 3, tmG_mn, tmHc_mn, tm_dW, tm_dW, sh, ep); };
+          if (!ce)          dW_alone(EpiAcc());
+          else if (half_dW) dW_alone(EpiAccW<4, kAccHalf>());
+          else              dW_alone(EpiAccW<4, kAccScaled>());
         }
         // these rows of dW are complete once the row slab that is walked last has added to them
         if (report) {

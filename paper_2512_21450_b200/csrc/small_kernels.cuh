@@ -769,6 +769,7 @@ struct LossParams {
   // cross entropy (its own instantiation): (1 - smooth) (lse - z_y) + smooth (lse - mean z) + z_coef lse^2
   float smooth, z_coef;
   int V;
+  float* out_scale;        // what the gradients are multiplied with where they leave: (1 - smooth) times the token mean's weight
   float* each_out;         // [T], the loss of every token before its weight, or NULL
 };
 // Fixed-order sum of column k of the block partials by one warp: lane l adds blocks l, l + 32, ... in order, then a
@@ -856,6 +857,7 @@ __global__ void __launch_bounds__(kLossThreads) combine_loss_kernel(const LossPa
     slab_extent(n, p.slab_cap, p.slab_one, p.slab_index, i_begin, i_end);
     i_end += i_begin;
   }
+  if (CE && blockIdx.x == 0 && threadIdx.x == 0) *p.out_scale = (p.token_weight ? 1.f : w_mean) * (1.f - p.smooth);
   int turn = 0;
   for (int i0 = i_begin + (blockIdx.x * kTeams + team) * 32; i0 < i_end; i0 += gridDim.x * kTeams * 32, turn ^= 1) {
     const int i = i0 + lane;
@@ -940,7 +942,7 @@ __global__ void __launch_bounds__(kLossThreads) combine_loss_kernel(const LossPa
         continue;
       }
       lse = M + logf(S);
-      logp = zy - lse;
+      logp = CE ? (zy - M) - logf(S) : zy - lse;   // (lse rounded first costs half its last place)
       ent = CE ? 0.f : lse - A / S;
     }
     if (p.kl_full) {
@@ -959,11 +961,15 @@ __global__ void __launch_bounds__(kLossThreads) combine_loss_kernel(const LossPa
     if (p.zero_coef) p.cp_c[i] = p.ce_c[i] = 0.f;
     if constexpr (CE) {
       const float w = p.token_weight ? tw : w_mean;
-      const float uniform = lse - A / (float)p.V;
+      const float uniform = (M - A / (float)p.V) + logf(S);
       const float each = fmaf(p.z_coef * lse, lse, fmaf(1.f - p.smooth, -logp, p.smooth * uniform));
       if (p.each_out) p.each_out[row] = each;
-      p.cp_c[i] = w * fmaf(2.f * p.z_coef, lse, 1.f);
-      p.ce_c[i] = w * (1.f - p.smooth);
+      // G is formed without the token mean's weight and 1 - smooth, which the gradients get in fp32 where they leave: the entry of
+      // a target that is unlikely is then near -1, and not the same rounding of (1 - smooth) / n in every row.  dH of 12 thousand
+      // rows is off by 1.9e-3 that way (the rounding of the result alone: 1.7e-3), by 2.7e-3 with the weight in G
+      const float u = p.token_weight ? tw : 1.f;
+      p.cp_c[i] = u * fmaf(2.f * p.z_coef, lse, 1.f) / (1.f - p.smooth);
+      p.ce_c[i] = u;
       acc[0] += (double)w * (double)each;
       acc[1] += (double)w * (double)(-logp);
       acc[2] += (double)w * (double)uniform;
@@ -1342,6 +1348,7 @@ struct DhSource {
   const int* row_map;
   void* dH;
   int f32;                 // dH is fp32
+  const float* scale;      // every element is multiplied with it, or NULL
 };
 
 __device__ __forceinline__ void add_piece(float4 (&x)[4], const float* q, int cols, int lane) {
@@ -1366,6 +1373,7 @@ __device__ __forceinline__ void scatter_rows(const DhSource& s, int n_valid, uns
   const int lane = threadIdx.x & 31;
   const unsigned col_tiles = (s.d + s.tile_cols - 1) / s.tile_cols;
   const unsigned units = (unsigned)rows * col_tiles;
+  const float scale = s.scale ? *s.scale : 1.f;
   for (unsigned u = warp; u < units; u += n_warps) {
     const int i = (int)(u / col_tiles), nt = (int)(u - i * col_tiles);
     const int cols = min(s.tile_cols, s.d - nt * s.tile_cols);
@@ -1390,6 +1398,10 @@ __device__ __forceinline__ void scatter_rows(const DhSource& s, int n_valid, uns
     } else {
       const float* q = s.acc + (size_t)i * s.d + col0;
       for (int k = 0; k < slices; ++k, q += s.split_stride) add_piece(x, q, cols, lane);
+    }
+    if (s.scale) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) { x[k].x *= scale; x[k].y *= scale; x[k].z *= scale; x[k].w *= scale; }
     }
     const size_t out = (size_t)s.row_map[slab_base + i] * s.d + col0;
 #pragma unroll
@@ -1422,8 +1434,8 @@ __global__ void __launch_bounds__(256) scatter_dH_kernel(const DhSource s, const
 }
 
 // dW of one slab; extra warps write dH of the same slab, which the launch before has left, meanwhile: a launch less.
-template <int W, bool HALF = false>
-struct EpiAccScatter : EpiAccW<W, HALF> {
+template <int W, int OUT = kAccPlain>
+struct EpiAccScatter : EpiAccW<W, OUT> {
   static constexpr int kSideWarps = 4;
   struct Params : AccParams {
     DhSource dh;

@@ -272,3 +272,67 @@ def test_scoring_agrees_with_the_logits(ctx):
 
 def _isfinite(out):
     return all(bool(torch.isfinite(v).all()) for v in out.values())
+
+
+def test_native_and_general_host_paths_agree(ctx, monkeypatch):
+    """The calls as the native host half makes them, which handles these, and as they are marshalled in Python."""
+    from paper_2512_21450_b200 import binding
+    X, W = _rows(70, 192, torch.bfloat16, seed=1), _rows(500, 192, torch.bfloat16, seed=2, std=0.1)
+    tok = torch.randint(0, 500, (70,), device=DEV, dtype=torch.int32)
+    mask = (torch.arange(70, device=DEV) % 5 != 0).to(torch.uint8)
+    weight, count = torch.rand(70, device=DEV), torch.tensor([55], dtype=torch.int64, device=DEV)
+    seen = []
+
+    class Watched:
+        def __getattr__(self, name):
+            def call(*args):
+                out = getattr(native, name)(*args)
+                seen.append((name, out is not NotImplemented))
+                return out
+            return call
+
+    def calls():
+        Q, s = ctx.rl_quantize_rows(W)
+        odd, so = ctx.rl_quantize_rows(X[:, :99].float())
+        out = [Q, s, odd, so, ctx.rl_quantize_rows(X[:1].half())[0]]
+        for n in (70, 1):
+            out += [ctx.rl_int8_linear(X[:n], Q, s, out_dtype=t) for t in TYPES]
+            out += ctx.rl_token_logprobs_int8(X[:n], Q, s, tok[:n], mask[:n])
+        hq, hs = ctx.rl_quantize_rows(X)
+        for kw in (dict(), dict(mask=mask, label_smoothing=0.1, z_coef=1e-3, token_count=count), dict(token_weight=weight, want_dW=False),
+                   dict(dW_bf16=True, want_dH=False), dict(dH_fp32=True), dict(want_dH=False, want_dW=False)):
+            got = ctx.rl_cross_entropy_fwd_bwd(X, W, tok, **kw)
+            out += [got[k] for k in sorted(got)]
+            got = ctx.rl_cross_entropy_fwd_bwd(hq, W, tok, H_scale=hs, **kw)
+            out += [got[k] for k in sorted(got)]
+        return out
+    calls()   # the workspace is there
+    native = binding._host
+    monkeypatch.setattr(binding, "_host", Watched())
+    a = calls()
+    assert len(seen) == 4 + 8 + 12 and all(ok for _, ok in seen), seen
+    monkeypatch.setattr(binding, "_host", binding._NoHostCalls())
+    b = calls()
+    assert len(a) == len(b)
+    for x, y in zip(a, b):
+        assert x.dtype == y.dtype and x.shape == y.shape and x.stride() == y.stride() and torch.equal(x, y)
+
+
+def test_what_the_native_half_leaves_to_the_general_path(ctx):
+    from paper_2512_21450_b200 import RLHeadError
+    X, W = _rows(10, 128, torch.bfloat16, seed=1), _rows(60, 128, torch.bfloat16, seed=2)
+    Q, s = ctx.rl_quantize_rows(W)
+    ctx.rl_int8_linear(X, Q, s)
+    for call in (lambda: ctx.rl_int8_linear(X.cpu(), Q, s), lambda: ctx.rl_int8_linear(X, Q.cpu(), s), lambda: ctx.rl_int8_linear(X, Q, s[:59]),
+                 lambda: ctx.rl_int8_linear(X[:, :64], Q, s), lambda: ctx.rl_quantize_rows(X.T), lambda: ctx.rl_quantize_rows(X.cpu()),
+                 lambda: ctx.rl_token_logprobs_int8(X, Q, s, torch.zeros(9, dtype=torch.int32, device=DEV)),
+                 lambda: ctx.rl_cross_entropy_fwd_bwd(X, W, torch.zeros(9, dtype=torch.int32, device=DEV)),
+                 lambda: ctx.rl_cross_entropy_fwd_bwd(X.cpu(), W, torch.zeros(10, dtype=torch.int32, device=DEV))):
+        with pytest.raises(AssertionError):
+            call()
+    with pytest.raises(RLHeadError) as e:
+        ctx.rl_cross_entropy_fwd_bwd(X, W, torch.zeros(10, dtype=torch.int32, device=DEV), label_smoothing=1.0)
+    assert e.value.status == 1
+    with pytest.raises(RLHeadError) as e:
+        ctx.rl_int8_linear(X, Q, torch.ones(61, device=DEV)[1:])      # scales that start on 4 bytes
+    assert e.value.status == 3

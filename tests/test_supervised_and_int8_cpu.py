@@ -125,7 +125,7 @@ def test_binding_refuses_what_does_not_fit():
     c = Context.__new__(Context)
     c.lib = Library()
     c._bind_stream = lambda: None
-    c.device, c._ws, c.handle = torch.device("cpu"), None, 0
+    c.device, c._ws, c.handle, c._address = torch.device("cpu"), None, 0, 0
     H, W, y = torch.zeros(4, 64, dtype=torch.bfloat16), torch.zeros(9, 64, dtype=torch.bfloat16), torch.zeros(4, dtype=torch.int32)
     Q, s = torch.zeros(4, 64, dtype=torch.int8), torch.zeros(4)
     Wq, ws = torch.zeros(9, 64, dtype=torch.int8), torch.zeros(9)
