@@ -100,9 +100,7 @@ __device__ __forceinline__ void load8(const T* row, int64_t k, int64_t d, float 
 template <class T, bool VEC>
 __global__ void __launch_bounds__(256) quantize_rows_kernel(const T* X, int64_t ldX, int64_t rows, int64_t d, int8_t* Q, int64_t ldQ,
                                                             float* scale) {
-  // released once everything before is done: a product that follows may read its other operand at once (StreamParams::early)
-  chain_wait();
-  chain_release();
+  chain_begin();
   const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
   for (int64_t r = (int64_t)blockIdx.x * warps + (threadIdx.x >> 5); r < rows; r += (int64_t)gridDim.x * warps) {
     const T* src = X + r * ldX;
@@ -191,6 +189,9 @@ struct ColumnScales {
 // 1682 / 2114 / 2486; fp32 logits 1211 / 1637 / 2113 / 2408 / 2835, 1080 / 1619 / 2087 / 2527 / 2966.
 constexpr int kEightWarpsStatsI8 = 2048;
 constexpr int kEightWarpsScale = 768;
+// Row by row (no TMA): 2048 rows x 50257 words, four / eight warps, bf16 227 / 171 us at d = 1024, 205 / 182 at 2048; fp32 192 / 216, 206 / 229.
+template <int OUT>
+constexpr int kWarpsByRow = OUT == 1 ? 4 : 8;
 
 // Statistics of RowStats over those logits: scoring under a head held in 8 bits.
 struct Int8StatsParams : RowStats::Params {
@@ -327,10 +328,16 @@ struct EpiScale {
         const int rows = min(32, m_rows - row0);
         if (col0 + lane < p.V) {
           size_t at = (size_t)row0 * p.ldC + col0 + lane;
-          for (int r = 0; r < rows; ++r, at += p.ldC) {
-            float x;
-            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(buf + r * 128u + ((uint32_t(lane >> 2) ^ uint32_t(r & 7)) << 4) + (lane & 3) * 4u) : "memory");
-            store_one<OUT>(p.C, at, x);
+          for (int r0 = 0; r0 < rows; r0 += 8) {   // eight loads on their way at a time
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int r = r0 + i;
+              asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x[i]) : "r"(buf + r * 128u + ((uint32_t(lane >> 2) ^ uint32_t(r & 7)) << 4) + (lane & 3) * 4u) : "memory");
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i, at += p.ldC)
+              if (r0 + i < rows) store_one<OUT>(p.C, at, x[i]);
           }
         }
         __syncwarp();   // before the next chunk takes the buffer
@@ -360,7 +367,6 @@ struct StreamParams {
   const float* a_scale;
   const float* b_scale;
   int T, V, k_blocks, rows, stages;   // rows of B per tile, at most 128
-  int early;   // the launch before this one is quantize_rows_kernel: whatever wrote B is done, and its first tiles are fetched meanwhile
   void* C;
   long long ldC;
 };
@@ -372,7 +378,7 @@ int8_stream_kernel(const __grid_constant__ CUtensorMap tmTokens, const __grid_co
   __shared__ uint32_t tmem_base_smem;
   __shared__ int abort_flag;
   __shared__ float a_s[4][N];   // a copy per warp
-  constexpr uint32_t kCols = 2 * N;   // two accumulators; a power of two from 32 on
+  constexpr uint32_t kCols = 2 * N <= 32 ? 32 : 2 * N <= 64 ? 64 : 128;   // two accumulators; a power of two from 32 on
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t tokens = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t ring = tokens + (uint32_t)p.k_blocks * N * 128u;
@@ -393,7 +399,7 @@ int8_stream_kernel(const __grid_constant__ CUtensorMap tmTokens, const __grid_co
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (!(p.early && warp == 0)) chain_wait();
+  chain_wait();
   const uint32_t tmem_base = tmem_base_smem;
   volatile int* abort_p = &abort_flag;
   const int r0 = (int)((long long)p.V * blockIdx.x / gridDim.x), r1 = (int)((long long)p.V * (blockIdx.x + 1) / gridDim.x);
@@ -402,20 +408,11 @@ int8_stream_kernel(const __grid_constant__ CUtensorMap tmTokens, const __grid_co
   if (warp == 0) {
     if (lane == 0) {
       const uint32_t tok_bar = smem_u32(&bar_tokens);
-      auto load_tokens = [&] {
-        mbar_arrive_expect_tx(tok_bar, (uint32_t)p.k_blocks * N * 128u);
-        for (int kb = 0; kb < p.k_blocks; ++kb) tma_load_2d(tokens + (uint32_t)kb * N * 128u, &tmTokens, tok_bar, kb * 128, 0);
-      };
+      mbar_arrive_expect_tx(tok_bar, (uint32_t)p.k_blocks * N * 128u);
+      for (int kb = 0; kb < p.k_blocks; ++kb) tma_load_2d(tokens + (uint32_t)kb * N * 128u, &tmTokens, tok_bar, kb * 128, 0);
       int stage = 0;
       uint32_t phase = 0;
       bool ok = true;
-      // the tokens once the ring is full, or first
-      const int n_early = p.early ? min(p.stages, p.k_blocks * tiles) : 0;
-      int issued = 0;
-      if (n_early == 0) {
-        chain_wait();
-        load_tokens();
-      }
       for (int t = 0; t < tiles && ok; ++t) {
         for (int kb = 0; kb < p.k_blocks; ++kb) {
           if (!mbar_wait_bounded(smem_u32(&bar_empty[stage]), phase ^ 1u, abort_p)) {
@@ -426,10 +423,6 @@ int8_stream_kernel(const __grid_constant__ CUtensorMap tmTokens, const __grid_co
           const uint32_t full = smem_u32(&bar_full[stage]);
           mbar_arrive_expect_tx(full, (uint32_t)p.rows * 128u);
           tma_load_2d(ring + (uint32_t)stage * kStreamStageBytes, &tmRows, full, kb * 128, r0 + t * p.rows);
-          if (++issued == n_early) {
-            chain_wait();
-            load_tokens();
-          }
           if (++stage == p.stages) { stage = 0; phase ^= 1u; }
         }
       }
@@ -508,7 +501,7 @@ int8_stream_kernel(const __grid_constant__ CUtensorMap tmTokens, const __grid_co
         tc_fence_after();
         const uint32_t taddr = tmem_base + a * N + (uint32_t(q * 32) << 16);
         size_t out = r >= 0 ? (size_t)r : 0;
-        constexpr int kStep = N < 32 ? 16 : 32;
+          constexpr int kStep = N % 32 ? 16 : 32;
 #pragma unroll 1
         for (int c = 0; c < N; c += kStep) {
           if (c >= p.T) break;

@@ -416,9 +416,9 @@ cudaError_t set_smem_attr_int8() {
   also(set_smem_attr<EpiScale<kOutBf16, true, 4>, 0, 0>());
   also(set_smem_attr<EpiScale<kOutF32, true, 4>, 0, 0>());
   also(set_smem_attr<EpiScale<kOutF16, true, 4>, 0, 0>());
-  also(set_smem_attr<EpiScale<kOutBf16, false, 4>, 0, 0>());
-  also(set_smem_attr<EpiScale<kOutF32, false, 4>, 0, 0>());
-  also(set_smem_attr<EpiScale<kOutF16, false, 4>, 0, 0>());
+  also(set_smem_attr<EpiScale<kOutBf16, false, kWarpsByRow<kOutBf16>>, 0, 0>());
+  also(set_smem_attr<EpiScale<kOutF32, false, kWarpsByRow<kOutF32>>, 0, 0>());
+  also(set_smem_attr<EpiScale<kOutF16, false, kWarpsByRow<kOutF16>>, 0, 0>());
   auto stream = [&](auto kernel) { also(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kStreamSmem)); };
   auto stream_out = [&](auto n) {
     constexpr int N = decltype(n)::value;
@@ -428,6 +428,7 @@ cudaError_t set_smem_attr_int8() {
   };
   stream_out(std::integral_constant<int, 16>());
   stream_out(std::integral_constant<int, 32>());
+  stream_out(std::integral_constant<int, 48>());
   stream_out(std::integral_constant<int, 64>());
   return e;
 }
@@ -554,7 +555,7 @@ rl_status int8_tiles(rl_ctx* c, const CUtensorMap& a, const CUtensorMap& b, int 
   // (the TMA unit clips a box at a row's end to 16 bytes: with a V that ends inside them, what lies behind would be written too)
   const bool tma = (reinterpret_cast<uintptr_t>(p.C) & 15) == 0 && p.ldC * kElem % 16 == 0 && (int64_t)p.V * kElem % 16 == 0;
   if (!tma) {
-    launch_gemm<EpiScale<OUT, false, 4>, 0, 0>(c, cg, 0, a, b, a, a, sh, p);
+    launch_gemm<EpiScale<OUT, false, kWarpsByRow<OUT>>, 0, 0>(c, cg, 0, a, b, a, a, sh, p);
     return cuda_ok();
   }
   CUtensorMap out;
@@ -1882,9 +1883,8 @@ static rl_status check_int8(const void* B, int64_t ldB, const float* b_scale, in
   return RL_OK;
 }
 
-// early: see StreamParams.
-static rl_status int8_matmul(rl_ctx* c, const int8_t* A, int64_t ldA, const float* a_scale, const int8_t* B, int64_t ldB,
-                             const float* b_scale, int64_t T, int64_t d, int64_t V, void* C, int c_dtype, int64_t ldC, int early) {
+rl_status rl_int8_matmul(rl_ctx* c, const int8_t* A, int64_t ldA, const float* a_scale, const int8_t* B, int64_t ldB, const float* b_scale,
+                         int64_t T, int64_t d, int64_t V, void* C, int c_dtype, int64_t ldC) {
   if (!c) return RL_ERR_INVALID_ARG;
   rl_status s = check_int8(B, ldB, b_scale, T, d, V, C, c_dtype, ldC);
   if (s != RL_OK) return s;
@@ -1893,9 +1893,9 @@ static rl_status int8_matmul(rl_ctx* c, const int8_t* A, int64_t ldA, const floa
   if (ldA < d) return RL_ERR_SHAPE;
   if ((reinterpret_cast<uintptr_t>(A) & 15) || ldA % 16 || (reinterpret_cast<uintptr_t>(a_scale) & 3)) return RL_ERR_ALIGNMENT;
   const OnDevice on(c);
-  const int k_blocks = (int)((d + 127) / 128), n_stream = T <= 16 ? 16 : T <= 32 ? 32 : 64;
+  const int k_blocks = (int)((d + 127) / 128), n_stream = T <= 16 ? 16 : T <= 32 ? 32 : T <= 48 ? 48 : 64;
   if (T <= 64 && stream_stages(n_stream, k_blocks) >= kStreamMinStages) {
-    StreamParams p = {a_scale, b_scale, (int)T, (int)V, k_blocks, 0, stream_stages(n_stream, k_blocks), early, C, ldC};
+    StreamParams p = {a_scale, b_scale, (int)T, (int)V, k_blocks, 0, stream_stages(n_stream, k_blocks), C, ldC};
     const int64_t per = (V + c->grid[1] - 1) / c->grid[1], tiles = (per + 127) / 128;
     p.rows = (int)((per + tiles - 1) / tiles);
     const int blocks = (int)(V < c->grid[1] ? V : c->grid[1]);
@@ -1911,6 +1911,7 @@ static rl_status int8_matmul(rl_ctx* c, const int8_t* A, int64_t ldA, const floa
     };
     if (n_stream == 16) go(std::integral_constant<int, 16>());
     else if (n_stream == 32) go(std::integral_constant<int, 32>());
+    else if (n_stream == 48) go(std::integral_constant<int, 48>());
     else go(std::integral_constant<int, 64>());
     prof_end(c, pr, 0);
     c->launches++;
@@ -1931,11 +1932,6 @@ static rl_status int8_matmul(rl_ctx* c, const int8_t* A, int64_t ldA, const floa
   const ScaleParams p = {a_scale, b_scale, (int)V, C, ldC};
   return c_dtype == RL_FP32 ? int8_tiles<kOutF32>(c, a, b, cg, sh, p, T)
          : c_dtype == RL_FP16 ? int8_tiles<kOutF16>(c, a, b, cg, sh, p, T) : int8_tiles<kOutBf16>(c, a, b, cg, sh, p, T);
-}
-
-rl_status rl_int8_matmul(rl_ctx* c, const int8_t* A, int64_t ldA, const float* a_scale, const int8_t* B, int64_t ldB, const float* b_scale,
-                         int64_t T, int64_t d, int64_t V, void* C, int c_dtype, int64_t ldC) {
-  return int8_matmul(c, A, ldA, a_scale, B, ldB, b_scale, T, d, V, C, c_dtype, ldC, 0);
 }
 
 // Quantised rows of int8_linear in the workspace, their scales behind them.
@@ -1959,7 +1955,7 @@ rl_status rl_int8_linear(rl_ctx* c, const void* X, int x_dtype, int64_t ldX, con
   float* a_scale = T > 0 ? reinterpret_cast<float*>(static_cast<char*>(c->ws) + int8_rows_bytes(T, d)) : nullptr;
   const int64_t ldA = (int64_t)align_up((size_t)d, 16);
   if ((s = rl_quantize_rows(c, X, x_dtype, ldX, T, d, A, ldA, a_scale)) != RL_OK || T == 0) return s;
-  return int8_matmul(c, A, ldA, a_scale, B, ldB, b_scale, T, d, V, C, c_dtype, ldC, 1);
+  return rl_int8_matmul(c, A, ldA, a_scale, B, ldB, b_scale, T, d, V, C, c_dtype, ldC);
 }
 
 rl_status rl_token_logprobs_int8(rl_ctx* c, const void* H, int64_t ldH, const int8_t* W, int64_t ldW, const float* w_scale,

@@ -100,7 +100,7 @@ def _int8(T, d, seed, lo=-128):
 
 PRODUCTS = [(1, 1, 1), (1, 64, 7), (2, 17, 33), (3, 2048, 1000), (4, 100, 515), (5, 33, 2), (8, 1000, 4099), (7, 8000, 300), (8, 8192, 77),
             (8, 8193, 65), (9, 64, 1), (9, 1, 300), (16, 129, 256), (128, 256, 1000), (129, 256, 1000), (200, 1000, 4099), (300, 2048, 513), (257, 127, 8),
-            (12, 3584, 40000), (33, 100, 1000), (40, 2048, 515), (64, 1024, 20011), (65, 130, 149), (100, 1024, 1500), (128, 900, 148), (17, 12000, 700)]
+            (12, 3584, 40000), (33, 100, 1000), (40, 2048, 515), (64, 1024, 20011), (65, 130, 149), (100, 1024, 1500), (128, 900, 148), (17, 12000, 700), (33, 2560, 900), (48, 3200, 151), (64, 2432, 333)]
 
 
 @pytest.mark.parametrize("T,d,V", PRODUCTS)
@@ -249,6 +249,48 @@ def test_scoring(ctx, T, d, V):
     assert_within(ent[on], E, dL + (p * z.abs()).sum(1) * 4 * (dz + 1e-6) + dz, "entropy")
     for x in (logp, ent, lse):
         assert bool((x[~on] == 0).all())
+
+
+@pytest.mark.parametrize("T", [100, 300])
+def test_scoring_nothing_that_counts(ctx, T):
+    """No valid row, before and after calls that have some: what a pass has fetched ahead is dropped."""
+    W = _rows(3000, 448, torch.bfloat16, seed=1, std=0.05)
+    H = _rows(T, 448, torch.bfloat16, seed=2)
+    tok = torch.randint(0, 3000, (T,), device=DEV, dtype=torch.int32)
+    Wq, ws = ctx.rl_quantize_rows(W)
+    want = [x.clone() for x in ctx.rl_token_logprobs_int8(H, Wq, ws, tok)]
+    for _ in range(3):
+        for x in ctx.rl_token_logprobs_int8(H, Wq, ws, tok, torch.zeros(T, dtype=torch.uint8, device=DEV)):
+            assert bool((x == 0).all())
+        one = torch.zeros(T, dtype=torch.uint8, device=DEV)
+        one[T - 1] = 1
+        for x, w in zip(ctx.rl_token_logprobs_int8(H, Wq, ws, tok, one), want):
+            assert abs((x[T - 1] - w[T - 1]).item()) <= 4e-6 * (1 + abs(w[T - 1].item())) and bool((x[:T - 1] == 0).all())
+        for x, w in zip(ctx.rl_token_logprobs_int8(H, Wq, ws, tok), want):
+            assert torch.equal(x, w)
+    assert ctx.rl_token_logprobs_int8(H[:0], Wq, ws, tok[:0])[0].shape == (0,)
+    _ok(ctx)
+
+
+def test_weights_written_just_before(ctx):
+    """The weights are fetched ahead of the tokens, but not ahead of the launch that writes them."""
+    base = [ctx.rl_quantize_rows(_rows(40000, 1024, torch.bfloat16, seed=s, std=0.05)) for s in (1, 2)]
+    H = _rows(100, 1024, torch.bfloat16, seed=3)
+    tok = torch.randint(0, 40000, (100,), device=DEV, dtype=torch.int32)
+    Wq, ws = torch.empty_like(base[0][0]), torch.empty_like(base[0][1])
+    calls = (lambda q, s: ctx.rl_int8_linear(H[:5], q, s), lambda q, s: ctx.rl_int8_linear(H, q, s),
+             lambda q, s: ctx.rl_token_logprobs_int8(H, q, s, tok)[0])
+    want = [[f(*b).clone() for b in base] for f in calls]
+    for f, w in zip(calls, want):
+        for i in (0, 1, 0, 1):
+            Wq.copy_(base[i][0]), ws.copy_(base[i][1])
+            assert torch.equal(f(Wq, ws), w[i])
+    # and by one of the library's own launches
+    X = [_rows(40000, 1024, torch.bfloat16, seed=s, std=0.05) for s in (1, 2)]
+    for f, w in zip(calls, want):
+        for i in (0, 1, 0, 1):
+            ctx.rl_quantize_rows(X[i], Q=Wq, scale=ws)
+            assert torch.equal(f(Wq, ws), w[i])
 
 
 def test_scoring_agrees_with_the_logits(ctx):
