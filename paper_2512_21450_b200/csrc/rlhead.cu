@@ -737,7 +737,7 @@ rl_status run_forward(rl_ctx* c, const WsLayout& L, const void* H, int64_t ldH, 
   sh.n_range = 0;  // split chosen on the device from the number of valid rows
   sh.n_split_max = L.part_ranges;
   sh.leaves_ranges = 1;
-  sh.m_group = row_group_tiles(c, d + (kl ? kl->d_ref : 0));
+  sh.m_group = row_group_tiles(c, plan.W_scale ? (d + 1) / 2 : d + (kl ? kl->d_ref : 0));
   RowStats::Params ep;
   ep.tokens_c = tokens_c;
   ep.partials = reinterpret_cast<float4*>(ws + L.partials);

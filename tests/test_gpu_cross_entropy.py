@@ -256,6 +256,80 @@ def test_captured_and_replayed(ctx):
         assert torch.equal(a, want[k]), k
 
 
+@pytest.mark.parametrize("limits", [(0, 0), (128, 0), (128, 512)])
+def test_accumulation_and_reports_over_slabs(limits):
+    """dW added to over several slabs, and its rows reported while the backward pass runs."""
+    from paper_2512_21450_b200 import Context
+    c = Context(0)
+    try:
+        c.set_slab_limits(*limits)
+        H, W, y, mask = _inputs(500, 960, 1300, seed=31, masked=0.3)
+        kw = dict(label_smoothing=0.1, z_coef=1e-3)
+        want, bound = cross_entropy(H, W, y, mask, 0.1, 1e-3)["dW"]
+        start = torch.randn(1300, 960, device=DEV) * 1e-3
+        dW = start.clone()
+        c.rl_cross_entropy_fwd_bwd(H, W, y, mask, accumulate_dW=True, dW=dW, **kw)
+        assert_within(dW, start.double() + want, bound + 2.0 ** -22 * (start.double().abs() + want.abs()), "dW")
+        seen = []
+        c.set_dw_slab_hook(lambda slab, a, b: seen.append((slab, a, b)))
+        got = c.rl_cross_entropy_fwd_bwd(H, W, y, mask, **kw)
+        assert [s for s, _, _ in seen] == list(range(len(seen))) and seen[0][1] == 0 and seen[-1][2] == 1300
+        assert all(a[2] == b[1] for a, b in zip(seen, seen[1:]))
+        assert_within(got["dW"], want, bound, "dW")
+        dW = start.clone()
+        c.rl_cross_entropy_fwd_bwd(H, W, y, mask, accumulate_dW=True, dW=dW, **kw)
+        assert_within(dW, start.double() + want, bound + 2.0 ** -22 * (start.double().abs() + want.abs()), "dW")
+    finally:
+        c.set_dw_slab_hook(None)
+        c.close()
+
+
+@pytest.mark.parametrize("options", [dict(cta_group=1), dict(wide_tiles=0), dict(dh_stream_k=1), dict(dh_k_slices=3), dict(max_ctas=6),
+                                     dict(row_group_bytes=1 << 20)])
+def test_options_of_the_context(options):
+    from paper_2512_21450_b200 import Context
+    c = Context(0)
+    try:
+        for name, value in options.items():
+            getattr(c, "set_" + name)(value)
+        H, W, y, mask = _inputs(600, 1024, 2100, seed=32, masked=0.2)
+        _check(c, H, W, y, mask, label_smoothing=0.1, z_coef=1e-3, dW_bf16=True)
+        _check(c, H, W, y, mask)
+        Wq, ws = c.rl_quantize_rows(W)
+        for T in (3, 90, 600):
+            q, s = c.rl_quantize_rows(H[:T])
+            z = (q.double() @ Wq.double().T).float() * s[:, None] * ws
+            assert torch.equal(c.rl_int8_linear(H[:T], Wq, ws, out_dtype=torch.float32), z)
+            lse = c.rl_token_logprobs_int8(H[:T], Wq, ws, y[:T])[2]
+            assert (lse - torch.logsumexp(z.double(), 1)).abs().max().item() <= 1e-6 * (lse.abs().max().item() + 12)
+    finally:
+        c.close()
+
+
+def test_between_calls_of_the_policy_loss(ctx):
+    """Calls of one context that share its workspace, in turn."""
+    H, W, y, mask = _inputs(300, 1024, 3000, seed=33, masked=0.2)
+    Wq, ws = ctx.rl_quantize_rows(W)
+    old, adv = torch.randn(300, device=DEV) - 8, torch.randn(300, device=DEV)
+    policy = lambda: ctx.rl_policy_loss_fwd_bwd(H, W, y, old, old, adv, mask, 0.2, 0.2, 0.04, ent_coef=1e-3)  # noqa: E731
+    others = (lambda: ctx.rl_cross_entropy_fwd_bwd(H, W, y, mask, label_smoothing=0.1, dW_bf16=True),
+              lambda: dict(zip("abc", ctx.rl_token_logprobs_int8(H, Wq, ws, y, mask))), lambda: dict(a=ctx.rl_int8_linear(H, Wq, ws)),
+              lambda: dict(zip("abc", ctx.rl_token_logprobs(H, W, y, mask))))
+    want_policy, want = policy(), [f() for f in others]
+    for f, w in zip(others, want):
+        for _ in range(2):
+            got = f()
+            assert all(torch.equal(got[k], w[k]) for k in w)
+            got = policy()
+            assert all(torch.equal(got[k], want_policy[k]) for k in want_policy)
+
+
+def test_twice_the_same(ctx):
+    H, W, y, mask = _inputs(700, 2048, 5000, seed=34, masked=0.3)
+    a, b = (ctx.rl_cross_entropy_fwd_bwd(H, W, y, mask, label_smoothing=0.1, z_coef=1e-4) for _ in range(2))
+    assert all(torch.equal(a[k], b[k]) for k in a)
+
+
 def test_token_out_of_range_is_reported(ctx):
     H, W, y, _ = _inputs(20, 64, 100)
     y[7] = 100
