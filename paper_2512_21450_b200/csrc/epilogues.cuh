@@ -389,7 +389,8 @@ struct AccParams {
   int slab_cap, slab_one, slab_index;
   int row_base;
   int slice_add;   // stream-K launches: output slices past the first are always added to
-  const float* scale;   // kAccScaled, kAccHalf: what every element is multiplied with
+  const float* scale;   // kAccScaled, kAccHalf, EpiAccSlabs: what every element is multiplied with
+  DevStatus* status;    // EpiAccSlabs
   int tile_cols;   // > 0: k_slice > 0 names slot k_slice - 1, a box of tile_cols columns x tile_rows rows of its own
   int tile_rows;
 };
@@ -476,5 +477,123 @@ struct EpiAccW {
   __device__ static __forceinline__ void end_unit(const Params&, State&, int, int, int, int) {}
 };
 using EpiAcc = EpiAccW<4>;
+
+// dW in bf16 that is added up over several slabs of rows: in fp32 (the second output map), until the slab that is the last to have rows,
+// which only the device knows, adds its own to what is there and stores bf16 (the first map).  What is there comes back through the TMA
+// unit, one 32 x 32 box per warp ahead, from L2, where it was sent for during the tile before.
+// Against a launch that rounds at the end, 12 thousand rows x 151936 words, d = 2048: the launch took 290 us.
+struct EpiAccSlabs {
+  static constexpr bool kParts = false, kTwoOut = true;
+  static constexpr int kSideWarps = 0;
+  static constexpr bool kFeeds = false, kAhead = true, kInt8 = false;
+  static constexpr int kWarps = 4;
+  static constexpr int kMerge = 0;
+  static constexpr int kStagingBytes = kEpiStaging;
+  using Params = AccParams;
+  struct State {
+    float scale;
+    int first, last;
+    uint32_t n_issued;   // boxes stored
+    uint32_t n_loaded;   // boxes fetched, of this warp's barrier
+    int next_row, next_col;   // this warp's part of the next tile (row -1: none)
+    bool lost;
+  };
+  __device__ static __forceinline__ uint64_t* bars() {
+    __shared__ __align__(8) uint64_t bar[kWarps];
+    return bar;
+  }
+  __device__ static __forceinline__ uint32_t bar() { return smem_u32(bars() + (threadIdx.x >> 5) - 2); }
+  __device__ static __forceinline__ void init(State& st) {
+    st.n_issued = st.n_loaded = 0;
+    st.lost = false;
+    if ((threadIdx.x & 31) == 0) {
+      mbar_init(bar(), 1);
+      fence_mbar_init();
+    }
+    __syncwarp();
+  }
+  __device__ static __forceinline__ void finish(State& st) {
+    if ((threadIdx.x & 31) == 0 && st.n_issued) bulk_wait_group_all();
+    if (st.lost)   // the copy given up on lands before the block's shared memory goes away
+      for (int it = 0; it < 4096 && !mbar_try_wait(bar(), st.n_loaded & 1u); ++it) {}
+    __syncwarp();
+  }
+  __device__ static __forceinline__ void begin_unit(const Params& p, State& st, int, int, int, int, int, int) {
+    st.scale = *p.scale;
+    st.first = p.slab_index == 0;
+    st.last = p.slab_index + 1 >= slab_count(*p.n_valid, p.slab_cap, p.slab_one);
+  }
+  __device__ static __forceinline__ void fetch(const CUtensorMap* map, uint32_t buf, int col, int row) {
+    mbar_arrive_expect_tx(bar(), kBoxBytes);
+    tma_load_3d(buf, map, bar(), col, row, 0);
+  }
+  __device__ static __forceinline__ void chunk(const Params& p, State& st, int m_tile, int n_tile, int c, int row_in_tile, int m_rows,
+                                               const float (&acc)[32], const CUtensorMap* tmC, const CUtensorMap* tmSum, uint32_t staging) {
+    const int lane = threadIdx.x & 31;
+    const int row0 = m_tile * BM + (row_in_tile - lane), col0 = n_tile * BN + c * 32;
+    if (row0 >= m_rows || col0 >= p.n_cols) return;   // warp-uniform
+    const int row = p.row_base + row0;
+    float v[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = acc[i] * st.scale;
+    if (!st.last) {
+      const uint32_t buf = staging + (st.n_issued % 2) * kBoxBytes;
+      if (lane == 0) bulk_wait_group_read<1>();
+      __syncwarp();
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t addr = buf + lane * 128u + (uint32_t((j ^ (lane & 7)) << 4));
+        asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(v[4 * j]), "f"(v[4 * j + 1]), "f"(v[4 * j + 2]),
+                     "f"(v[4 * j + 3])
+                     : "memory");
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        if (st.first) tma_store_3d(tmSum, buf, col0, row, 0);
+        else          tma_reduce_add_3d(tmSum, buf, col0, row, 0);
+        bulk_commit_group();
+      }
+      st.n_issued++;
+      return;
+    }
+    if (!st.first) {
+      if (st.lost) return;
+      if (lane == 0) {
+        if (c == 0) fetch(tmSum, staging, col0, row);
+        if (st.next_row >= 0 && st.next_row < m_rows && st.next_col + c * 32 < p.n_cols)
+          tma_prefetch_3d(tmSum, st.next_col + c * 32, p.row_base + st.next_row, 0);
+      }
+      __syncwarp();
+      bool here = false;
+      for (int it = 0; it < (1 << 22) && !here; ++it) here = mbar_try_wait(bar(), st.n_loaded & 1u) != 0;
+      if (!__all_sync(0xffffffffu, here)) {
+        if (lane == 0) latch_status(p.status, kStatusTimeout, (6 << 28) | (blockIdx.x << 8) | 0xfd);
+        st.lost = true;
+        return;
+      }
+      st.n_loaded++;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        float4 q;
+        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+                     : "=f"(q.x), "=f"(q.y), "=f"(q.z), "=f"(q.w)
+                     : "r"(staging + lane * 128u + (uint32_t((j ^ (lane & 7)) << 4)))
+                     : "memory");
+        v[4 * j] += q.x; v[4 * j + 1] += q.y; v[4 * j + 2] += q.z; v[4 * j + 3] += q.w;
+      }
+      __syncwarp();
+      if (lane == 0 && c + 1 < BN / 32 && col0 + 32 < p.n_cols) fetch(tmSum, staging, col0 + 32, row);
+    }
+    uint32_t w[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&b);
+    }
+    stage_half_box<1>(w, c, staging + kBoxBytes, st.n_issued, tmC, col0, row);
+  }
+  __device__ static __forceinline__ void end_unit(const Params&, State&, int, int, int, int) {}
+};
 
 }  // namespace rlh

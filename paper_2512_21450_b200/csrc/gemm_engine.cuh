@@ -51,6 +51,8 @@
 #pragma once
 #include <cuda.h>
 
+#include <type_traits>
+
 #include "ptx.cuh"
 
 namespace rlh {
@@ -74,7 +76,7 @@ constexpr int kMinShare = 8;    // least k-blocks of a part of a cut tile
 constexpr int kPartCost = 20;   // k-blocks in whose time the output of one part leaves the chip (cut_tiles)
 constexpr int kHelpSplit = 16;  // most parts per cut tile for which the workers left over are given work (cut_tiles)
 constexpr int kFwdRange = 8;    // column tiles per work unit when there is plenty of work
-// K-blocks up to which an epilogue is told where this worker's next tile lies (Epi::kAhead): with more, the products take longer
+// K-blocks up to which an epilogue that only adds is told where this worker's next tile lies (Epi::kAhead): with more, the products take longer
 // than the output, and prefetches only get in the way.
 constexpr int kAheadBlocks = 10;
 // An A operand that is formed while it is read (Epi::kFeeds): a job is kFeedRows rows x kFeedCols columns (of K).
@@ -480,9 +482,14 @@ struct UnitWalk {
 //   if kFeeds:
 //     static bool feeds(const Params&, const GemmExtents&, int n_workers);   // or A is complete when the launch starts
 //     static const unsigned* feed_flag(const Params&, int m_tile, int chunk);
+//   static constexpr bool kTwoOut (may be left out): chunk receives the second output map, that of the parts, behind the first.
 //   kTileDual: chunk receives the chunk of the second product as well (..., v, v2, out_map, staging).
 // m_tile counts 128-row tiles, n_tile 256-column tiles (a wide tile n covers column tiles 2n and 2n + 1;
 // sh.n_tiles then counts 512-wide tiles).  tmA2 / tmB2 / k2_len are read by kTileDual only.
+template <class Epi, class = void>
+struct TwoOut : std::false_type {};
+template <class Epi>
+struct TwoOut<Epi, std::enable_if_t<Epi::kTwoOut>> : std::true_type {};
 template <class Epi, int A_MN, int B_MN, int CG, int MODE>
 __global__ void __launch_bounds__(gemm_threads(Epi::kWarps, Epi::kSideWarps, Epi::kFeeds), 1)
 gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
@@ -788,7 +795,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
       if constexpr (Epi::kAhead) {
         UnitWalk peek = walk;
         int mu2, nr2, ks2, lo2, hi2;
-        const bool more = ex.k_blocks <= kAheadBlocks && peek.next(mu2, nr2, ks2, lo2, hi2);
+        const bool more = (ex.k_blocks <= kAheadBlocks || TwoOut<Epi>::value) && peek.next(mu2, nr2, ks2, lo2, hi2);
         st.next_row = more ? (mu2 * CG + (int)rank) * BM + q * 32 : -1;
         st.next_col = more ? nr2 * BN : 0;
       }
@@ -832,8 +839,11 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
 #pragma unroll
                 for (int i = 0; i < 32; ++i) v[i] = 0.f;
               }
-              Epi::chunk(ep, st, m, n * Cfg::kBBoxes + s, c, row_in_tile, ex.m_rows, v,
-                         Epi::kParts && ex.stream_k == 2 && ks > 0 ? part_map : &tmC, staging);
+              if constexpr (TwoOut<Epi>::value)
+                Epi::chunk(ep, st, m, n * Cfg::kBBoxes + s, c, row_in_tile, ex.m_rows, v, &tmC, part_map, staging);
+              else
+                Epi::chunk(ep, st, m, n * Cfg::kBBoxes + s, c, row_in_tile, ex.m_rows, v,
+                           Epi::kParts && ex.stream_k == 2 && ks > 0 ? part_map : &tmC, staging);
             }
           }
           if (has_k) {

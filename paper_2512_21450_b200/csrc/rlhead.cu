@@ -308,9 +308,9 @@ size_t ws_bytes(const rl_ctx* c, int64_t T, int64_t d, int64_t V) {
   return twice > L.total ? twice : L.total;
 }
 
-// Of a cross entropy; round_dW: dW is added up in fp32 behind everything else.
-inline size_t ce_ws_bytes(const WsLayout& L, int64_t d, int64_t V, bool round_dW) {
-  return round_dW ? align_up(L.total, 1024) + (size_t)V * d * 4 : L.total;
+// Of a cross entropy; sum_dW: dW is added up in fp32 behind everything else.
+inline size_t ce_ws_bytes(const WsLayout& L, int64_t d, int64_t V, bool sum_dW) {
+  return sum_dW ? align_up(L.total, 1024) + (size_t)V * d * 4 : L.total;
 }
 
 // K-major operand: global tensor [rows, k] with k contiguous, row stride ld elements.
@@ -621,16 +621,6 @@ struct CeArgs {
   const float* H_scale;   // H in 8 bits
 };
 
-// fp32 -> bf16, eight values per thread and step: dW that was added up over several slabs.
-__global__ void __launch_bounds__(256) round_bf16_kernel(const float4* __restrict__ x, uint4* __restrict__ y, long long n8) {
-  chain_begin();
-  for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n8; i += (long long)gridDim.x * blockDim.x) {
-    const float4 a = __ldcs(x + 2 * i), b = __ldcs(x + 2 * i + 1);
-    __stcs(y + i, make_uint4(two_halves<kOutBf16>(a.x, a.y), two_halves<kOutBf16>(a.z, a.w), two_halves<kOutBf16>(b.x, b.y),
-                             two_halves<kOutBf16>(b.z, b.w)));
-  }
-}
-
 // Compute capability and SM count (cudaGetDeviceProperties takes 2.5 ms, these two queries a microsecond).
 rl_status device_facts(int device, int* major, int* n_sm) {
   if (cudaDeviceGetAttribute(major, cudaDevAttrComputeCapabilityMajor, device) != cudaSuccess ||
@@ -855,7 +845,8 @@ rl_status rl_create(rl_ctx** out, int device) {
             set_smem_attr_one<EpiAccFedOf<kGradCE>, 0, 1, 2, kTileWide>() == cudaSuccess &&
             set_smem_attr<EpiAccW<4, kAccHalf>, 1, 1>() == cudaSuccess && set_smem_attr<EpiAccScatter<4, kAccHalf>, 1, 1>() == cudaSuccess &&
             set_smem_attr<EpiAccScatter<8, kAccHalf>, 1, 1>() == cudaSuccess && set_smem_attr<EpiAccW<4, kAccScaled>, 1, 1>() == cudaSuccess &&
-            set_smem_attr<EpiAccScatter<4, kAccScaled>, 1, 1>() == cudaSuccess && set_smem_attr<EpiAccScatter<8, kAccScaled>, 1, 1>() == cudaSuccess && set_smem_attr_int8() == cudaSuccess;
+            set_smem_attr<EpiAccScatter<4, kAccScaled>, 1, 1>() == cudaSuccess && set_smem_attr<EpiAccScatter<8, kAccScaled>, 1, 1>() == cudaSuccess && set_smem_attr<EpiAccSlabs, 1, 1>() == cudaSuccess &&
+            set_smem_attr<EpiScatterWith<EpiAccSlabs>, 1, 1>() == cudaSuccess && set_smem_attr_int8() == cudaSuccess;
   if (!ok) { cudaFree(c->dstatus); delete c; return RL_ERR_CUDA; }
   {
     // how many CTA pairs can be resident at once (pairs must share a TPC): the persistent grid
@@ -1347,8 +1338,8 @@ static rl_status loss_fwd_bwd_impl(rl_ctx* c, const void* H, int64_t ldH, const 
   if (seq_path && L.n_row_slabs > 1) L = ws_layout(c, T, d, V, 0, 0, true);
   const bool backward = dH || dW;
   // dW in bf16 is written where it is formed, unless it is added up over several slabs: then in fp32 behind everything else
-  const bool round_dW = dW && ce && ce->dW_bf16 && L.n_row_slabs > 1, half_dW = ce && ce->dW_bf16 && !round_dW;
-  if ((s = check_ws(c, !backward && T > 0 ? L.G : ce_ws_bytes(L, d, V, round_dW))) != RL_OK) return s;
+  const bool sum_dW = dW && ce && ce->dW_bf16 && L.n_row_slabs > 1, half_dW = ce && ce->dW_bf16 && !sum_dW;
+  if ((s = check_ws(c, !backward && T > 0 ? L.G : ce_ws_bytes(L, d, V, sum_dW))) != RL_OK) return s;
   char* ws = static_cast<char*>(c->ws);
   cudaStream_t st = c->stream;
 
@@ -1490,7 +1481,6 @@ static rl_status loss_fwd_bwd_impl(rl_ctx* c, const void* H, int64_t ldH, const 
   };
   if (!sweep) merge_and_loss(0);
   if (!backward) return cuda_ok();
-  float* dW_f32 = round_dW ? reinterpret_cast<float*>(ws + align_up(L.total, 1024)) : dW;
   // ---- backward, one (row slab x vocabulary slab) at a time
   __nv_bfloat16* Hc = reinterpret_cast<__nv_bfloat16*>(ws + L.Hc);
   __nv_bfloat16* G = reinterpret_cast<__nv_bfloat16*>(ws + L.G);
@@ -1499,7 +1489,7 @@ static rl_status loss_fwd_bwd_impl(rl_ctx* c, const void* H, int64_t ldH, const 
   const int* n_valid = &c->dstatus->n_valid;
 
   CUtensorMap tmHc_k, tmW_k, tmG_k, tmW_mn, tmG_mn, tmHc_mn, tm_dH, tm_dW, tm_G_out, tmHr_k, tmWr_k, tm_slots, tmW_fwd,
-      tmWr_fwd, tm_planes;
+      tmWr_fwd, tm_planes, tm_dW_sum;
   if (o.kl_full) {
     if (!map_kmajor(c, &tmHr_k, ws + L.Hc_ref, (uint64_t)L.Tpad, (uint64_t)o.d_ref, (uint64_t)o.d_ref, BM) ||
         !map_kmajor(c, &tmWr_k, o.W_ref, (uint64_t)V, (uint64_t)o.d_ref, (uint64_t)o.ldW_ref, b_box_rows(c)))
@@ -1513,8 +1503,11 @@ static rl_status loss_fwd_bwd_impl(rl_ctx* c, const void* H, int64_t ldH, const 
             map_mnmajor(c, &tmHc_mn, Hc, (uint64_t)L.Tpad, (uint64_t)d, (uint64_t)d, b_box_panels(c)) &&
             map_out_bf16(c, &tm_G_out, G, (uint64_t)L.Ts, (uint64_t)L.Vs, (uint64_t)L.Vs) &&
             map_out_f32(c, &tm_dH, dH_acc, (uint64_t)L.Ts, (uint64_t)d, (uint64_t)d, (uint64_t)dh_buffers(c), (uint64_t)L.Ts) &&
-            (!dW || (half_dW ? map_out_bf16(c, &tm_dW, dW, (uint64_t)V, (uint64_t)d, (uint64_t)d)
-                             : map_out_f32(c, &tm_dW, dW_f32, (uint64_t)V, (uint64_t)d, (uint64_t)d, 1, (uint64_t)V)));
+            (!dW || (half_dW || sum_dW ? map_out_bf16(c, &tm_dW, dW, (uint64_t)V, (uint64_t)d, (uint64_t)d)
+                                       : map_out_f32(c, &tm_dW, dW, (uint64_t)V, (uint64_t)d, (uint64_t)d, 1, (uint64_t)V)));
+  tm_dW_sum = tm_dW;
+  if (sum_dW)
+    ok = ok && map_out_f32(c, &tm_dW_sum, reinterpret_cast<float*>(ws + align_up(L.total, 1024)), (uint64_t)V, (uint64_t)d, (uint64_t)d, 1, (uint64_t)V);
   const int dh_tile_rows = BM * c->cta_group, dh_cols = dh_tile_cols(c, d);
   const int dh_workers = c->grid[c->cta_group] / c->cta_group;
   float* dH_slots = reinterpret_cast<float*>(ws + L.dH_slots);
@@ -1750,24 +1743,27 @@ static rl_status loss_fwd_bwd_impl(rl_ctx* c, const void* H, int64_t ldH, const 
         ep.n_valid = n_valid; ep.slab_cap = L.Tc; ep.slab_one = L.Ts; ep.slab_index = r;
         ep.row_base = vocab_base + c0; ep.slice_add = 0; ep.tile_cols = 0;
         ep.scale = p.out_scale;
+        ep.status = c->dstatus;
         if (dH_beside && !report && cs == n_col_slabs - 1) {
           src.shape = dh_shape;
           auto dW_and_dH = [&](auto epi) {
             typename decltype(epi)::Params es = {};
             static_cast<AccParams&>(es) = ep;
             es.dh = src;
-            launch_gemm<decltype(epi), 1, 1>(c, c->cta_group, 3, tmG_mn, tmHc_mn, tm_dW, tm_dW, sh, es);
+            launch_gemm<decltype(epi), 1, 1>(c, c->cta_group, 3, tmG_mn, tmHc_mn, tm_dW, tm_dW_sum, sh, es);
           };
           // (a worker with one or two tiles has nothing for more epilogue warps to overlap: the smallest step 52.2 -> 52.9 us)
           const long long tiles = (long long)d_tiles * ((cols + BN - 1) / BN);
           const bool eight = T <= kFewRows && tiles >= 4 * dh_workers;
           auto by_warps = [&](auto four, auto more) { eight ? dW_and_dH(more) : dW_and_dH(four); };
           if (!ce)          by_warps(EpiAccScatter<4>(), EpiAccScatter<8>());
+          else if (sum_dW)  dW_and_dH(EpiScatterWith<EpiAccSlabs>());
           else if (half_dW) by_warps(EpiAccScatter<4, kAccHalf>(), EpiAccScatter<8, kAccHalf>());
           else              by_warps(EpiAccScatter<4, kAccScaled>(), EpiAccScatter<8, kAccScaled>());
         } else {
-          auto dW_alone = [&](auto epi) { launch_gemm<decltype(epi), 1, 1>(c, c->cta_group, 3, tmG_mn, tmHc_mn, tm_dW, tm_dW, sh, ep); };
+          auto dW_alone = [&](auto epi) { launch_gemm<decltype(epi), 1, 1>(c, c->cta_group, 3, tmG_mn, tmHc_mn, tm_dW, tm_dW_sum, sh, ep); };
           if (!ce)          dW_alone(EpiAcc());
+          else if (sum_dW)  dW_alone(EpiAccSlabs());
           else if (half_dW) dW_alone(EpiAccW<4, kAccHalf>());
           else              dW_alone(EpiAccW<4, kAccScaled>());
         }
@@ -1787,14 +1783,6 @@ static rl_status loss_fwd_bwd_impl(rl_ctx* c, const void* H, int64_t ldH, const 
       prof_end(c, pr_sc, 7);
       c->launches++;
     }
-  }
-  if (round_dW) {
-    const long long n8 = (long long)V * d / 8, blocks = (n8 + 255) / 256;
-    const int pr_rd = prof_begin(c, 3);
-    launch(c, round_bf16_kernel, (int)(blocks < c->n_sm * 16 ? blocks : c->n_sm * 16), 256, reinterpret_cast<const float4*>(dW_f32),
-           reinterpret_cast<uint4*>(dW), n8);
-    prof_end(c, pr_rd, 3);
-    c->launches++;
   }
   return cuda_ok();
 }

@@ -1434,8 +1434,8 @@ __global__ void __launch_bounds__(256) scatter_dH_kernel(const DhSource s, const
 }
 
 // dW of one slab; extra warps write dH of the same slab, which the launch before has left, meanwhile: a launch less.
-template <int W, int OUT = kAccPlain>
-struct EpiAccScatter : EpiAccW<W, OUT> {
+template <class Acc>
+struct EpiScatterWith : Acc {
   static constexpr int kSideWarps = 4;
   struct Params : AccParams {
     DhSource dh;
@@ -1444,6 +1444,8 @@ struct EpiAccScatter : EpiAccW<W, OUT> {
     scatter_rows(p.dh, *p.n_valid, blockIdx.x * kSideWarps + warp, gridDim.x * kSideWarps);
   }
 };
+template <int W, int OUT = kAccPlain>
+using EpiAccScatter = EpiScatterWith<EpiAccW<W, OUT>>;
 
 // ------------------------------------------------------------------------------------------
 // Exercises the bounded waits, each with a short limit: on an mbarrier that nothing ever arrives on, on a counter in global memory and

@@ -324,6 +324,25 @@ def test_between_calls_of_the_policy_loss(ctx):
             assert all(torch.equal(got[k], want_policy[k]) for k in want_policy)
 
 
+@pytest.mark.parametrize("limits,T,d,V", [((128, 0), 700, 960, 1800), ((256, 512), 700, 192, 1800), ((0, 0), 500, 1024, 2000), ((128, 0), 3000, 2048, 600),
+                                          ((0, 0), 8000, 1024, 151936)])
+def test_bf16_dW_is_the_fp32_one_rounded(limits, T, d, V):
+    """However many slabs it is added up over."""
+    from paper_2512_21450_b200 import Context
+    c = Context(0)
+    try:
+        c.set_slab_limits(*limits)
+        H, W, y, mask = _inputs(T, d, V, seed=35, masked=0.1, std=0.02)
+        for m in (mask, torch.cat([mask[:T // 3], torch.zeros_like(mask[T // 3:])])):     # the last slabs have rows, or none
+            a = c.rl_cross_entropy_fwd_bwd(H, W, y, m, label_smoothing=0.1, z_coef=1e-4)["dW"].bfloat16()
+            for want_dH in (True, False):
+                b = c.rl_cross_entropy_fwd_bwd(H, W, y, m, label_smoothing=0.1, z_coef=1e-4, dW_bf16=True, want_dH=want_dH)["dW"]
+                assert torch.equal(a, b)
+            assert c.last_device_status()[0] == 0
+    finally:
+        c.close()
+
+
 def test_twice_the_same(ctx):
     H, W, y, mask = _inputs(700, 2048, 5000, seed=34, masked=0.3)
     a, b = (ctx.rl_cross_entropy_fwd_bwd(H, W, y, mask, label_smoothing=0.1, z_coef=1e-4) for _ in range(2))
