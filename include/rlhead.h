@@ -449,7 +449,7 @@ rl_status rl_token_logprobs_static(void* cuda_stream, const void* H, int64_t ldH
  * w_t = mask_t / sum(mask) unless opts say otherwise.  targets[T] int32 (rows with mask 0 are left out whatever they hold, and get 0
  * in every output); everything else as in rl_policy_loss_fwd_bwd.  dH or dW may be NULL: a gradient nobody needs (a frozen trunk or a
  * frozen head) is not formed.  dW is [V,d] fp32 or bf16, dH [T,d] bf16 or fp32.  Logits exist for one bounded slab of rows at a time,
- * in fp32 (rl_set_slab_limits).  Workspace: rl_workspace_bytes_ce (a bf16 dW of a call of several slabs is added up in fp32);
+ * in fp32 (rl_set_slab_limits).  Workspace: rl_workspace_bytes_ce (a bf16 dW of a call of several slabs is summed in fp32 there);
  * with neither gradient rl_workspace_bytes_logprobs.
  * H may be stored in 8 bits (rl_quantize_rows): opts->H_scale[T] then holds the scales, H points to int8_t, ldH counts bytes and is a
  * multiple of 16; the rows stand for bf16(H_scale[t] * H[t,k]) and dH is the gradient of those.

@@ -274,7 +274,10 @@ def _check(status, where):
 
 
 class Context:
-    """One library context on one device; owns a torch-allocated workspace."""
+    """One library context on one device; owns a torch-allocated workspace.  A workspace that calls were captured with into a CUDA graph
+    stays allocated as long as the context does, also when a larger one takes its place: the graph writes to it at every replay."""
+
+    _captured, _kept = False, ()   # whether calls were captured with the present workspace; earlier ones that calls were captured with
 
     def __init__(self, device=0):
         if not torch.cuda.is_available():
@@ -305,9 +308,20 @@ class Context:
         # the raw handle of torch's current stream, without building a Stream object for every call; the context keeps the
         # one it was given last
         stream = torch._C._cuda_getCurrentRawStream(self.device.index)
+        if torch._C._cuda_isCurrentStreamCapturing():
+            self._captured = True
         if stream != self._stream:
             _check(self.lib.rl_set_stream(self.handle, stream), "rl_set_stream")
             self._stream = stream
+
+    def _need_workspace(self, nbytes):
+        if self._ws is None or self._ws.numel() < nbytes:
+            if self._captured and self._ws is not None:
+                self._kept += (self._ws,)
+            self._captured = bool(torch._C._cuda_isCurrentStreamCapturing())
+            self._ws = None
+            self._ws = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=self.device)
+        _check(self.lib.rl_set_workspace(self.handle, _ptr(self._ws), self._ws.numel()), "rl_set_workspace")
 
     def workspace_bytes(self, T, d, V, host=False, d_ref=0, scoring=False):
         n = c_size_t()
@@ -320,11 +334,7 @@ class Context:
         return n.value
 
     def ensure_workspace(self, T, d, V, host=False, d_ref=0, scoring=False):
-        need = self.workspace_bytes(T, d, V, host, d_ref, scoring)
-        if self._ws is None or self._ws.numel() < need:
-            self._ws = None
-            self._ws = torch.empty(need, dtype=torch.uint8, device=self.device)
-        _check(self.lib.rl_set_workspace(self.handle, _ptr(self._ws), self._ws.numel()), "rl_set_workspace")
+        self._need_workspace(self.workspace_bytes(T, d, V, host, d_ref, scoring))
 
     def set_slab_limits(self, max_rows=0, max_cols=0):
         _check(self.lib.rl_set_slab_limits(self.handle, max_rows, max_cols), "rl_set_slab_limits")
@@ -530,7 +540,7 @@ class Context:
         _check_array(dW, V * d, dW_type)
         assert not (accumulate_dW and dW is None), "accumulate_dW adds to a dW that is given"
         need = c_size_t()
-        if want_dH or want_dW or T == 0:
+        if want_dH or want_dW:
             _check(self.lib.rl_workspace_bytes_ce(self.handle, T, d, V, DTYPES[dW_type if want_dW else torch.float32], byref(need)),
                    "rl_workspace_bytes_ce")
         else:
@@ -551,12 +561,6 @@ class Context:
             self.handle, _ptr(H), _row_stride(H) if H_scale is None else _row_stride_i8(H), _ptr(W), _row_stride(W), _ptr(targets),
             _ptr(mask), T, d, V, _ptr(out["loss"]), _ptr(out.get("dH")), _ptr(out.get("dW")), byref(opts)), "rl_cross_entropy_fwd_bwd")
         return out
-
-    def _need_workspace(self, nbytes):
-        if self._ws is None or self._ws.numel() < nbytes:
-            self._ws = None
-            self._ws = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=self.device)
-        _check(self.lib.rl_set_workspace(self.handle, _ptr(self._ws), self._ws.numel()), "rl_set_workspace")
 
     # ------------------------------------------------------------------ 8-bit rows
     def rl_quantize_rows(self, X, Q=None, scale=None):
@@ -694,9 +698,7 @@ class Context:
         self._bind_stream()
         T = mask.numel() if T is None else T
         need = (T // 4096 + 3) * 4
-        if self._ws is None or self._ws.numel() < need:
-            self._ws = torch.empty(max(need, 1 << 20), dtype=torch.uint8, device=self.device)
-        _check(self.lib.rl_set_workspace(self.handle, _ptr(self._ws), self._ws.numel()), "rl_set_workspace")
+        self._need_workspace(need if self._ws is not None and self._ws.numel() >= need else max(need, 1 << 20))
         if row_map is None:
             row_map = torch.empty(max(T, 1), dtype=torch.int32, device=self.device)
         if n_valid is None:
@@ -857,9 +859,7 @@ class Context:
                "rl_workspace_bytes_host_pipelined")
         if self._ws is None or self._ws.numel() < need.value:
             assert not any(self._slot_busy), "workspace must not be replaced while a step is in flight"
-            self._ws = None
-            self._ws = torch.empty(need.value, dtype=torch.uint8, device=self.device)
-        _check(self.lib.rl_set_workspace(self.handle, _ptr(self._ws), self._ws.numel()), "rl_set_workspace")
+        self._need_workspace(need.value)
         _check(self.lib.rl_policy_loss_fwd_bwd_host_submit(
             self.handle, slot, _ptr(H_host), d, _ptr(W), W.stride(0), _ptr(tokens_host), _ptr(old_host), _ptr(ref_host),
             _ptr(adv_host), _ptr(rewards_host), rewards_host.numel() if rewards_host is not None else 0, group_size,

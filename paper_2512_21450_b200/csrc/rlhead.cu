@@ -549,8 +549,7 @@ inline rl_status cuda_ok() { return cudaGetLastError() == cudaSuccess ? RL_OK : 
 
 // Product of 8-bit rows on the tensor cores; C through the TMA unit where its rows start and end on 16 bytes.
 template <int OUT>
-rl_status int8_tiles(rl_ctx* c, const CUtensorMap& a, const CUtensorMap& b, int cg, const GemmShape& sh, const ScaleParams& p,
-                            int64_t T) {
+rl_status int8_tiles(rl_ctx* c, const CUtensorMap& a, const CUtensorMap& b, int cg, const GemmShape& sh, const ScaleParams& p, int64_t T) {
   constexpr int kElem = OUT == kOutF32 ? 4 : 2;
   // (the TMA unit clips a box at a row's end to 16 bytes: with a V that ends inside them, what lies behind would be written too)
   const bool tma = (reinterpret_cast<uintptr_t>(p.C) & 15) == 0 && p.ldC * kElem % 16 == 0 && (int64_t)p.V * kElem % 16 == 0;
@@ -612,7 +611,7 @@ void launch_merge(rl_ctx* c, const LossParams& p, int64_t rows, int ranges, int 
   c->launches++;
 }
 
-// A call of the cross entropy (cross_entropy_impl): what it has besides the arguments of the loss calls.
+// A call of the cross entropy: what it has besides the arguments of the loss calls (loss_fwd_bwd_impl).
 struct CeArgs {
   float smooth, z_coef;
   float* lse_out;
@@ -1339,7 +1338,7 @@ static rl_status loss_fwd_bwd_impl(rl_ctx* c, const void* H, int64_t ldH, const 
   const bool backward = dH || dW;
   // dW in bf16 is written where it is formed, unless it is added up over several slabs: then in fp32 behind everything else
   const bool sum_dW = dW && ce && ce->dW_bf16 && L.n_row_slabs > 1, half_dW = ce && ce->dW_bf16 && !sum_dW;
-  if ((s = check_ws(c, !backward && T > 0 ? L.G : ce_ws_bytes(L, d, V, sum_dW))) != RL_OK) return s;
+  if ((s = check_ws(c, backward ? ce_ws_bytes(L, d, V, sum_dW) : L.G)) != RL_OK) return s;
   char* ws = static_cast<char*>(c->ws);
   cudaStream_t st = c->stream;
 

@@ -220,6 +220,42 @@ def test_streams_and_graphs(ctx):
     assert torch.equal(got, ctx.rl_int8_linear(X2, Wq, ws))
 
 
+def test_graphs_outlive_their_workspace():
+    """Two graphs of one context, captured at different sizes, the second with a workspace that took the first's place; replayed in turn,
+    with other memory written in between."""
+    from paper_2512_21450_b200 import Context
+    c = Context(0)
+    try:
+        X, W = _rows(300, 512, torch.bfloat16, seed=7), _rows(1000, 512, torch.bfloat16, seed=8)
+        tok = torch.randint(0, 1000, (300,), device=DEV, dtype=torch.int32)
+        Wq, ws = c.rl_quantize_rows(W)
+        C = torch.empty(5, 1000, dtype=torch.bfloat16, device=DEV)
+        dW = torch.empty(1000, 512, device=DEV)
+        small = lambda: c.rl_int8_linear(X[:5], Wq, ws, out=C)  # noqa: E731
+        large = lambda: c.rl_cross_entropy_fwd_bwd(X, W, tok, dW=dW)  # noqa: E731
+        want = small().clone()
+        graphs, addresses = [], []
+        for call in (small, large):
+            call()
+            addresses.append(c._ws.data_ptr())
+            torch.cuda.synchronize()
+            graphs.append(torch.cuda.CUDAGraph())
+            with torch.cuda.graph(graphs[-1]):
+                call()
+        want_dW = dW.clone()
+        c.rl_cross_entropy_fwd_bwd(torch.cat([X] * 4), W, torch.cat([tok] * 4))
+        assert [w.data_ptr() for w in c._kept] == addresses and c._ws.data_ptr() not in addresses
+        others = [torch.full((n,), 3.0, device=DEV) for n in (64, 1 << 12, 1 << 16, 1 << 20, 1 << 22) for _ in range(3)]
+        for _ in range(2):
+            C.zero_(), dW.zero_()
+            graphs[0].replay()
+            graphs[1].replay()
+            torch.cuda.synchronize()
+            assert torch.equal(C, want) and torch.equal(dW, want_dW) and all(bool((x == 3).all()) for x in others)
+    finally:
+        c.close()
+
+
 # ------------------------------------------------------------------ scoring
 @pytest.mark.parametrize("T,d,V", [(1, 64, 1), (1, 64, 300), (77, 192, 1000), (128, 2048, 3000), (129, 1024, 777), (700, 2176, 1500), (2000, 256, 5000)])
 def test_scoring(ctx, T, d, V):
