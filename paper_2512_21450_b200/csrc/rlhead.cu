@@ -426,6 +426,9 @@ cudaError_t set_smem_attr_int8() {
     stream(int8_stream_kernel<N, kOutF32>);
     stream(int8_stream_kernel<N, kOutF16>);
   };
+  stream(int8_stream_kernel<kStreamOwn, kOutBf16, true>);
+  stream(int8_stream_kernel<kStreamOwn, kOutF32, true>);
+  stream(int8_stream_kernel<kStreamOwn, kOutF16, true>);
   stream_out(std::integral_constant<int, 16>());
   stream_out(std::integral_constant<int, 32>());
   stream_out(std::integral_constant<int, 48>());
@@ -1870,6 +1873,47 @@ static rl_status check_int8(const void* B, int64_t ldB, const float* b_scale, in
   return RL_OK;
 }
 
+// Few tokens: the N side of the stream's tiles, and whether they fit beside a ring.
+static inline int stream_tokens(int64_t T) { return T <= 16 ? 16 : T <= 32 ? 32 : T <= 48 ? 48 : 64; }
+static inline bool streams(int64_t T, int64_t d) { return T <= 64 && stream_stages(stream_tokens(T), (int)((d + 127) / 128)) >= kStreamMinStages; }
+
+// tokens == NULL: p.X has them in bf16.
+static rl_status int8_stream(rl_ctx* c, const CUtensorMap* tokens, StreamParams p, const int8_t* B, int64_t ldB, const float* b_scale,
+                             int64_t T, int64_t d, int64_t V, void* C, int c_dtype, int64_t ldC) {
+  const int n = stream_tokens(T);
+  p.b_scale = b_scale;
+  p.T = (int)T;
+  p.V = (int)V;
+  p.d = (int)d;
+  p.k_blocks = (int)((d + 127) / 128);
+  p.stages = stream_stages(n, p.k_blocks);
+  p.C = C;
+  p.ldC = ldC;
+  const int64_t per = (V + c->grid[1] - 1) / c->grid[1], tiles = (per + 127) / 128;
+  p.rows = (int)((per + tiles - 1) / tiles);
+  const int blocks = (int)(V < c->grid[1] ? V : c->grid[1]);
+  CUtensorMap w;
+  if (!map_kmajor_i8(c, &w, B, (uint64_t)V, (uint64_t)d, (uint64_t)ldB, (uint32_t)p.rows)) return RL_ERR_CUDA;
+  const int pr = prof_begin(c, 0);
+  auto go = [&](int threads, auto bf16, auto f32, auto f16) {
+    launch_smem(c, c_dtype == RL_FP32 ? f32 : c_dtype == RL_FP16 ? f16 : bf16, blocks, threads, kStreamSmem, tokens ? *tokens : w, w, p, c->dstatus);
+  };
+  auto of = [&](auto n_) {
+    constexpr int N = decltype(n_)::value;
+    go(kStreamThreads, int8_stream_kernel<N, kOutBf16>, int8_stream_kernel<N, kOutF32>, int8_stream_kernel<N, kOutF16>);
+  };
+  if (!tokens)
+    go(kStreamThreads + 32 * kStreamOwnWarps, int8_stream_kernel<kStreamOwn, kOutBf16, true>, int8_stream_kernel<kStreamOwn, kOutF32, true>,
+       int8_stream_kernel<kStreamOwn, kOutF16, true>);
+  else if (n == 16) of(std::integral_constant<int, 16>());
+  else if (n == 32) of(std::integral_constant<int, 32>());
+  else if (n == 48) of(std::integral_constant<int, 48>());
+  else of(std::integral_constant<int, 64>());
+  prof_end(c, pr, 0);
+  c->launches++;
+  return cuda_ok();
+}
+
 rl_status rl_int8_matmul(rl_ctx* c, const int8_t* A, int64_t ldA, const float* a_scale, const int8_t* B, int64_t ldB, const float* b_scale,
                          int64_t T, int64_t d, int64_t V, void* C, int c_dtype, int64_t ldC) {
   if (!c) return RL_ERR_INVALID_ARG;
@@ -1880,29 +1924,12 @@ rl_status rl_int8_matmul(rl_ctx* c, const int8_t* A, int64_t ldA, const float* a
   if (ldA < d) return RL_ERR_SHAPE;
   if ((reinterpret_cast<uintptr_t>(A) & 15) || ldA % 16 || (reinterpret_cast<uintptr_t>(a_scale) & 3)) return RL_ERR_ALIGNMENT;
   const OnDevice on(c);
-  const int k_blocks = (int)((d + 127) / 128), n_stream = T <= 16 ? 16 : T <= 32 ? 32 : T <= 48 ? 48 : 64;
-  if (T <= 64 && stream_stages(n_stream, k_blocks) >= kStreamMinStages) {
-    StreamParams p = {a_scale, b_scale, (int)T, (int)V, k_blocks, 0, stream_stages(n_stream, k_blocks), C, ldC};
-    const int64_t per = (V + c->grid[1] - 1) / c->grid[1], tiles = (per + 127) / 128;
-    p.rows = (int)((per + tiles - 1) / tiles);
-    const int blocks = (int)(V < c->grid[1] ? V : c->grid[1]);
-    CUtensorMap x, w;
-    if (!map_kmajor_i8(c, &x, A, (uint64_t)T, (uint64_t)d, (uint64_t)ldA, (uint32_t)n_stream) ||
-        !map_kmajor_i8(c, &w, B, (uint64_t)V, (uint64_t)d, (uint64_t)ldB, (uint32_t)p.rows))
-      return RL_ERR_CUDA;
-    const int pr = prof_begin(c, 0);
-    auto go = [&](auto n) {
-      constexpr int N = decltype(n)::value;
-      auto kernel = c_dtype == RL_FP32 ? int8_stream_kernel<N, kOutF32> : c_dtype == RL_FP16 ? int8_stream_kernel<N, kOutF16> : int8_stream_kernel<N, kOutBf16>;
-      launch_smem(c, kernel, blocks, kStreamThreads, kStreamSmem, x, w, p, c->dstatus);
-    };
-    if (n_stream == 16) go(std::integral_constant<int, 16>());
-    else if (n_stream == 32) go(std::integral_constant<int, 32>());
-    else if (n_stream == 48) go(std::integral_constant<int, 48>());
-    else go(std::integral_constant<int, 64>());
-    prof_end(c, pr, 0);
-    c->launches++;
-    return cuda_ok();
+  if (streams(T, d)) {
+    StreamParams p = {};
+    p.a_scale = a_scale;
+    CUtensorMap x;
+    if (!map_kmajor_i8(c, &x, A, (uint64_t)T, (uint64_t)d, (uint64_t)ldA, (uint32_t)stream_tokens(T))) return RL_ERR_CUDA;
+    return int8_stream(c, &x, p, B, ldB, b_scale, T, d, V, C, c_dtype, ldC);
   }
   const int cg = T <= BM ? 1 : c->cta_group;
   CUtensorMap a, b;
@@ -1937,6 +1964,15 @@ rl_status rl_int8_linear(rl_ctx* c, const void* X, int x_dtype, int64_t ldX, con
   if (s != RL_OK) return s;
   if (T > 0) {
     if ((s = check_ws(c, int8_rows_bytes(T, d) + (size_t)T * 4)) != RL_OK) return s;
+  }
+  // few tokens in bf16 are quantised where they are used
+  if (T > 0 && T <= kStreamOwn && x_dtype == RL_BF16 && streams(T, d) && X && ldX >= d && d % 8 == 0 && ldX % 8 == 0 &&
+      (reinterpret_cast<uintptr_t>(X) & 15) == 0) {
+    const OnDevice on(c);
+    StreamParams p = {};
+    p.X = static_cast<const __nv_bfloat16*>(X);
+    p.ldX = ldX;
+    return int8_stream(c, nullptr, p, B, ldB, b_scale, T, d, V, C, c_dtype, ldC);
   }
   int8_t* A = static_cast<int8_t*>(c->ws);
   float* a_scale = T > 0 ? reinterpret_cast<float*>(static_cast<char*>(c->ws) + int8_rows_bytes(T, d)) : nullptr;

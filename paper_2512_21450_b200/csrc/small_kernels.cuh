@@ -212,7 +212,7 @@ __device__ __forceinline__ void prep_row(const PrepParams& p, int t, int pos, in
     for (int v = lane; v < p.d / 16; v += 32) unpack16(__ldg(q + v), s, dst[2 * v], dst[2 * v + 1]);
   } else if constexpr (KIND == kRowsToInt8) {
     uint2* q = reinterpret_cast<uint2*>(reinterpret_cast<int8_t*>(p.Hc) + (size_t)pos * p.d);
-    const float s = quantize_row_bf16(src, vec_per_row, q, lane);
+    const float s = quantize_row_bf16<8>(src, vec_per_row, lane, [&](int v, uint2 w) { q[v] = w; });
     if (lane == 0) p.scale_c[pos] = s;
   } else {
 #pragma unroll 8

@@ -143,7 +143,8 @@ def test_largest_sums(ctx, T):
 
 
 @pytest.mark.parametrize("x_dtype", TYPES)
-@pytest.mark.parametrize("T,d,V", [(1, 2048, 1001), (6, 100, 300), (33, 1000, 4099), (300, 512, 777)])
+@pytest.mark.parametrize("T,d,V", [(1, 2048, 1001), (6, 100, 300), (33, 1000, 4099), (300, 512, 777), (1, 8, 1), (2, 136, 149), (12, 1000, 515),
+                                   (13, 3584, 20000), (16, 4104, 333), (16, 10000, 300), (3, 7, 50), (17, 640, 2000)])
 def test_linear(ctx, x_dtype, T, d, V):
     X, W = _rows(T, d, x_dtype, seed=1), _rows(V, d, torch.bfloat16, seed=2, std=0.05)
     Wq, ws = ctx.rl_quantize_rows(W)
