@@ -6,8 +6,9 @@
  * log-probability of every sampled token under the next-token policy over the vocabulary
  * (section 2.2), its entropy (section 2.2 "Regularization"), the clipped importance-ratio
  * surrogate (section 3.1) with a KL-to-reference regulariser, and the gradient of the resulting
- * loss with respect to the hidden states H and the LM-head weight W.  The [T,V] logits are
- * never written to memory.
+ * loss with respect to the hidden states H and the LM-head weight W.  On the same head: the
+ * supervised cross entropy with its gradients, rows kept in 8 bits, and a head held in 8-bit
+ * integers.  Only the calls whose result they are (rl_int8_matmul, rl_int8_linear) write [T,V] logits.
  *
  * Conventions
  *   - Unless a parameter says "host", every pointer is a DEVICE pointer owned by the caller.

@@ -220,7 +220,7 @@ def _load_host_calls(lib):
     host.bind(*(ctypes.cast(getattr(lib, name), c_void_p).value for name in (
         "rl_workspace_bytes", "rl_workspace_bytes_logprobs", "rl_set_workspace", "rl_grpo_advantages_ex", "rl_kl_shaped_returns",
         "rl_token_loss", "rl_token_logprobs", "rl_policy_loss_fwd_bwd_ex", "rl_workspace_bytes_ce", "rl_cross_entropy_fwd_bwd",
-        "rl_quantize_rows", "rl_workspace_bytes_int8_linear", "rl_int8_linear", "rl_token_logprobs_int8")))
+        "rl_quantize_rows", "rl_workspace_bytes_int8_linear", "rl_int8_linear", "rl_int8_matmul", "rl_token_logprobs_int8")))
     _host = host
 
 
@@ -594,6 +594,10 @@ class Context:
     def rl_int8_matmul(self, A, a_scale, Wq, w_scale, out_dtype=torch.bfloat16, out=None):
         """[T, V] = a_scale[t] w_scale[v] sum_k A[t, k] Wq[v, k] of 8-bit rows (rl_quantize_rows)."""
         self._bind_stream()
+        if out is None and out_dtype in DTYPES:
+            got = _host.int8_matmul(self._address, self.device.index, A, a_scale, Wq, w_scale, DTYPES[out_dtype])
+            if _handled(got, "rl_int8_matmul"):
+                return got[0]
         T, d = A.shape
         assert A.dtype == torch.int8 and Wq.shape[1] == d
         _check_array(a_scale, T)

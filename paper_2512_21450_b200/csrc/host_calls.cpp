@@ -26,6 +26,7 @@ struct Abi {
   decltype(&rl_quantize_rows) quantize_rows;
   decltype(&rl_workspace_bytes_int8_linear) workspace_bytes_int8_linear;
   decltype(&rl_int8_linear) int8_linear;
+  decltype(&rl_int8_matmul) int8_matmul;
   decltype(&rl_token_logprobs_int8) token_logprobs_int8;
 } abi;
 
@@ -403,6 +404,30 @@ PyObject* int8_linear(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   });
 }
 
+// (context, device, A, a_scale, Wq, w_scale, out_dtype) -> (product,)
+PyObject* int8_matmul(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  return guarded([&](Outputs& out) {
+    Args a(args, nargs, 7);
+    rl_ctx* c = a.context();
+    a.device = a.small();
+    const at::Tensor* A = a.rows(at::kChar);
+    const int64_t T = A->size(0), d = A->size(1);
+    if (T == 0) throw General();
+    const at::Tensor *a_scale = a.values(T, false), *W = a.rows(at::kChar);
+    const int64_t V = W->size(0);
+    if (W->size(1) != d) throw General();
+    const at::Tensor* scale = a.values(V, false);
+    const int out_type = a.small();
+    if (out_type < 0 || out_type > 2) throw General();
+    const int8_t *pa = data<int8_t>(A), *pw = data<int8_t>(W);
+    const float *pas = data<float>(a_scale), *ps = data<float>(scale);
+    const int64_t ldA = row_stride(A, 16), ldW = row_stride(W, 16);
+    Unlocked u;
+    void* C = out.add(at::empty({T, V}, A->options().dtype(kTypes[out_type]).requires_grad(false)));
+    return abi.int8_matmul(c, pa, ldA, pas, pw, ldW, ps, T, d, V, C, out_type, V);
+  });
+}
+
 // (context, device, workspace, H, Wq, w_scale, tokens, mask) -> (logp, entropy, lse)
 PyObject* token_logprobs_int8(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   return guarded([&](Outputs& out) {
@@ -453,6 +478,7 @@ PyMethodDef methods[] = {
     {"cross_entropy", reinterpret_cast<PyCFunction>(cross_entropy), METH_FASTCALL, nullptr},
     {"quantize_rows", reinterpret_cast<PyCFunction>(quantize_rows), METH_FASTCALL, nullptr},
     {"int8_linear", reinterpret_cast<PyCFunction>(int8_linear), METH_FASTCALL, nullptr},
+    {"int8_matmul", reinterpret_cast<PyCFunction>(int8_matmul), METH_FASTCALL, nullptr},
     {"token_logprobs_int8", reinterpret_cast<PyCFunction>(token_logprobs_int8), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

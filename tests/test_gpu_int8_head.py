@@ -257,6 +257,41 @@ def test_graphs_outlive_their_workspace():
         c.close()
 
 
+def test_two_contexts_at_once():
+    """Contexts of two threads on two streams, their kernels side by side."""
+    import threading
+    from paper_2512_21450_b200 import Context
+    X, W = _rows(600, 1024, torch.bfloat16, seed=7), _rows(9000, 1024, torch.bfloat16, seed=8, std=0.05)
+    tok = torch.randint(0, 9000, (600,), device=DEV, dtype=torch.int32)
+    torch.cuda.synchronize()
+    made, wrong = {}, []
+
+    def work(i):
+        c = Context(0)
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            for turn in range(6):
+                Wq, ws = c.rl_quantize_rows(W)
+                got = [c.rl_int8_linear(X[:n], Wq, ws) for n in (1, 40, 600)] + list(c.rl_token_logprobs_int8(X, Wq, ws, tok))
+                ce = c.rl_cross_entropy_fwd_bwd(X, W, tok, label_smoothing=0.1, dW_bf16=True)
+                got += [ce["loss"], ce["dH"], ce["dW"]]
+                stream.synchronize()
+                if turn == 0:
+                    made[i] = got
+                elif not all(torch.equal(a, b) for a, b in zip(got, made[i])):
+                    wrong.append((i, turn))
+        if c.last_device_status()[0] != 0:
+            wrong.append((i, "status"))
+        c.close()
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong and len(made) == 2 and all(torch.equal(a, b) for a, b in zip(made[0], made[1]))
+
+
 # ------------------------------------------------------------------ scoring
 @pytest.mark.parametrize("T,d,V", [(1, 64, 1), (1, 64, 300), (77, 192, 1000), (128, 2048, 3000), (129, 1024, 777), (700, 2176, 1500), (2000, 256, 5000)])
 def test_scoring(ctx, T, d, V):
@@ -378,6 +413,7 @@ def test_native_and_general_host_paths_agree(ctx, monkeypatch):
             out += [ctx.rl_int8_linear(X[:n], Q, s, out_dtype=t) for t in TYPES]
             out += ctx.rl_token_logprobs_int8(X[:n], Q, s, tok[:n], mask[:n])
         hq, hs = ctx.rl_quantize_rows(X)
+        out += [ctx.rl_int8_matmul(hq[:n], hs[:n], Q, s, out_dtype=t) for n in (70, 1) for t in TYPES]
         for kw in (dict(), dict(mask=mask, label_smoothing=0.1, z_coef=1e-3, token_count=count), dict(token_weight=weight, want_dW=False),
                    dict(dW_bf16=True, want_dH=False), dict(dH_fp32=True), dict(want_dH=False, want_dW=False)):
             got = ctx.rl_cross_entropy_fwd_bwd(X, W, tok, **kw)
@@ -389,7 +425,7 @@ def test_native_and_general_host_paths_agree(ctx, monkeypatch):
     native = binding._host
     monkeypatch.setattr(binding, "_host", Watched())
     a = calls()
-    assert len(seen) == 4 + 8 + 12 and all(ok for _, ok in seen), seen
+    assert len(seen) == 4 + 8 + 6 + 12 and all(ok for _, ok in seen), seen
     monkeypatch.setattr(binding, "_host", binding._NoHostCalls())
     b = calls()
     assert len(a) == len(b)
@@ -403,7 +439,8 @@ def test_what_the_native_half_leaves_to_the_general_path(ctx):
     Q, s = ctx.rl_quantize_rows(W)
     ctx.rl_int8_linear(X, Q, s)
     for call in (lambda: ctx.rl_int8_linear(X.cpu(), Q, s), lambda: ctx.rl_int8_linear(X, Q.cpu(), s), lambda: ctx.rl_int8_linear(X, Q, s[:59]),
-                 lambda: ctx.rl_int8_linear(X[:, :64], Q, s), lambda: ctx.rl_quantize_rows(X.T), lambda: ctx.rl_quantize_rows(X.cpu()),
+                 lambda: ctx.rl_int8_linear(X[:, :64], Q, s), lambda: ctx.rl_int8_matmul(Q, s[:9], Q, s), lambda: ctx.rl_int8_matmul(Q[:, :64], s, Q, s),
+                 lambda: ctx.rl_int8_matmul(X, s[:10], Q, s), lambda: ctx.rl_quantize_rows(X.T), lambda: ctx.rl_quantize_rows(X.cpu()),
                  lambda: ctx.rl_token_logprobs_int8(X, Q, s, torch.zeros(9, dtype=torch.int32, device=DEV)),
                  lambda: ctx.rl_cross_entropy_fwd_bwd(X, W, torch.zeros(9, dtype=torch.int32, device=DEV)),
                  lambda: ctx.rl_cross_entropy_fwd_bwd(X.cpu(), W, torch.zeros(10, dtype=torch.int32, device=DEV))):
