@@ -378,112 +378,173 @@ struct StreamParams {
   void* C;
   long long ldC;
 };
-template <int N, int OUT, bool OWN = false>
-__global__ void __launch_bounds__(kStreamThreads + (OWN ? 32 * kStreamOwnWarps : 0), 1)
-int8_stream_kernel(const __grid_constant__ CUtensorMap tmTokens, const __grid_constant__ CUtensorMap tmRows, const StreamParams p, DevStatus* status) {
-  extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t bar_full[kStreamMaxStages], bar_empty[kStreamMaxStages], bar_acc_full[2], bar_acc_empty[2], bar_tokens, bar_drain;
-  __shared__ uint32_t tmem_base_smem;
-  __shared__ int abort_flag;
-  __shared__ float a_s[4][N];   // a copy per warp
-  constexpr uint32_t kCols = 2 * N <= 32 ? 32 : 2 * N <= 64 ? 64 : 128;   // two accumulators; a power of two from 32 on
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t tokens = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  const uint32_t ring = tokens + (uint32_t)p.k_blocks * N * 128u;
+// What both kernels of the stream share: barriers, the producer, the issuer of the products.
+struct StreamBars {
+  uint64_t full[kStreamMaxStages], empty[kStreamMaxStages], acc_full[2], acc_empty[2], tokens, drain;
+  uint32_t tmem_base;
+  int abort_flag;
+};
+template <int N>
+constexpr uint32_t kStreamCols = 2 * N <= 32 ? 32 : 2 * N <= 64 ? 64 : 128;   // two accumulators; a power of two from 32 on
+// Before the launch's memory is touched.  acc_warps: warps that read an accumulator; token_arrivals: on the barrier of the tokens.
+template <int N>
+__device__ __forceinline__ void stream_begin(StreamBars& s, const CUtensorMap* tmTokens, const CUtensorMap* tmRows, int acc_warps, int token_arrivals) {
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kStreamMaxStages; ++s) { mbar_init(smem_u32(&bar_full[s]), 1); mbar_init(smem_u32(&bar_empty[s]), 1); }
-    for (int a = 0; a < 2; ++a) { mbar_init(smem_u32(&bar_acc_full[a]), 1); mbar_init(smem_u32(&bar_acc_empty[a]), 4); }
-    mbar_init(smem_u32(&bar_tokens), OWN ? 4 + kStreamOwnWarps : 1);
-    mbar_init(smem_u32(&bar_drain), 1);
-    abort_flag = 0;
+    for (int i = 0; i < kStreamMaxStages; ++i) { mbar_init(smem_u32(&s.full[i]), 1); mbar_init(smem_u32(&s.empty[i]), 1); }
+    for (int a = 0; a < 2; ++a) { mbar_init(smem_u32(&s.acc_full[a]), 1); mbar_init(smem_u32(&s.acc_empty[a]), acc_warps); }
+    mbar_init(smem_u32(&s.tokens), token_arrivals);
+    mbar_init(smem_u32(&s.drain), 1);
+    s.abort_flag = 0;
     fence_mbar_init();
-    if (!OWN) prefetch_tmap(&tmTokens);
-    prefetch_tmap(&tmRows);
+    prefetch_tmap(tmTokens);
+    prefetch_tmap(tmRows);
   }
-  if (warp == 1) {
-    tmem_alloc(smem_u32(&tmem_base_smem), kCols);
+  if (threadIdx.x >> 5 == 1) {
+    tmem_alloc(smem_u32(&s.tmem_base), kStreamCols<N>);
     tmem_relinquish();
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   chain_wait();
-  const uint32_t tmem_base = tmem_base_smem;
-  volatile int* abort_p = &abort_flag;
+}
+template <int N>
+__device__ __forceinline__ void stream_end(StreamBars& s) {
+  chain_release();
+  tc_fence_before();
+  __syncthreads();
+  if (threadIdx.x >> 5 == 1) {
+    __syncwarp();
+    tc_fence_after();
+    tmem_dealloc(s.tmem_base, kStreamCols<N>);
+  }
+}
+// One thread.  tmTokens NULL: others put the tokens where they belong.
+template <int N>
+__device__ __forceinline__ void stream_produce(StreamBars& s, const CUtensorMap* tmTokens, const CUtensorMap* tmRows, const StreamParams& p, uint32_t tokens,
+                                               uint32_t ring, int r0, int tiles, DevStatus* status) {
+  const uint32_t tok_bar = smem_u32(&s.tokens);
+  if (tmTokens) {
+    mbar_arrive_expect_tx(tok_bar, (uint32_t)p.k_blocks * N * 128u);
+    for (int kb = 0; kb < p.k_blocks; ++kb) tma_load_2d(tokens + (uint32_t)kb * N * 128u, tmTokens, tok_bar, kb * 128, 0);
+  }
+  int stage = 0;
+  uint32_t phase = 0;
+  bool ok = true;
+  for (int t = 0; t < tiles && ok; ++t) {
+    for (int kb = 0; kb < p.k_blocks; ++kb) {
+      if (!mbar_wait_bounded(smem_u32(&s.empty[stage]), phase ^ 1u, &s.abort_flag)) {
+        latch_status(status, kStatusTimeout, (1 << 28) | (blockIdx.x << 8) | stage);
+        ok = false;
+        break;
+      }
+      const uint32_t full = smem_u32(&s.full[stage]);
+      mbar_arrive_expect_tx(full, (uint32_t)p.rows * 128u);
+      tma_load_2d(ring + (uint32_t)stage * kStreamStageBytes, tmRows, full, kb * 128, r0 + t * p.rows);
+      if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+    }
+  }
+  if (!ok) {
+    // copies already issued land before the block's shared memory goes away
+    for (int i = 0; i < p.stages; ++i) {
+      const uint32_t ph = i < stage ? phase : (phase ^ 1u);
+      for (int it = 0; it < 4096 && !mbar_try_wait(smem_u32(&s.full[i]), ph); ++it) {}
+    }
+    for (int it = 0; tmTokens && it < 4096 && !mbar_try_wait(tok_bar, 0); ++it) {}
+  }
+}
+// One thread.
+template <int N>
+__device__ __forceinline__ void stream_multiply(StreamBars& s, const StreamParams& p, uint32_t tokens, uint32_t ring, int tiles, DevStatus* status) {
+  constexpr uint32_t idesc = make_idesc_s8(128, N);
+  constexpr uint64_t hi = make_smem_desc_hi(16, 1024);
+  constexpr uint32_t hi32 = uint32_t(hi >> 32), lo_const = uint32_t(hi);
+  const uint32_t ring_lo = (ring & 0x3FFFFu) >> 4, tok_lo = (tokens & 0x3FFFFu) >> 4, tmem_base = s.tmem_base;
+  int stage = 0;
+  uint32_t phase = 0;
+  bool ok = tiles == 0 || mbar_wait_bounded(smem_u32(&s.tokens), 0, &s.abort_flag);
+  if (!ok) latch_status(status, kStatusTimeout, (3 << 28) | (blockIdx.x << 8) | 0xff);
+  for (int t = 0; t < tiles && ok; ++t) {
+    const uint32_t a = t & 1u;
+    if (!mbar_wait_bounded(smem_u32(&s.acc_empty[a]), ((t >> 1) & 1u) ^ 1u, &s.abort_flag)) {
+      latch_status(status, kStatusTimeout, (2 << 28) | (blockIdx.x << 8) | a);
+      ok = false;
+      break;
+    }
+    tc_fence_after();
+    for (int kb = 0; kb < p.k_blocks; ++kb) {
+      if (!mbar_wait_bounded(smem_u32(&s.full[stage]), phase, &s.abort_flag)) {
+        latch_status(status, kStatusTimeout, (3 << 28) | (blockIdx.x << 8) | stage);
+        ok = false;
+        break;
+      }
+      tc_fence_after();
+      const uint32_t w = lo_const | (ring_lo + (uint32_t)stage * (kStreamStageBytes >> 4)), x = lo_const | (tok_lo + (uint32_t)kb * (N * 128 >> 4));
+#pragma unroll
+      for (int k = 0; k < 4; ++k) umma_i8_words<1>(tmem_base + a * N, w + 2 * k, hi32, x + 2 * k, hi32, idesc, (kb > 0 || k > 0) ? 1u : 0u);
+      umma_commit(smem_u32(&s.empty[stage]));
+      if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+    }
+    if (ok) umma_commit(smem_u32(&s.acc_full[a]));
+  }
+  umma_commit(smem_u32(&s.drain));
+  bool drained = false;
+  for (int it = 0; it < (1 << 22) && !drained; ++it) drained = mbar_try_wait(smem_u32(&s.drain), 0) != 0;
+  if (!drained) latch_status(status, kStatusTimeout, (4 << 28) | (blockIdx.x << 8));
+}
+// The accumulators of this block's tiles, one after the other, by one warp: of(tile u of four, row of B or -1, its scale, accumulator's address).
+// Scales of rows are loaded four tiles early: while the ring streams B such a load takes as long as a tile or two.
+template <int N, class Of>
+__device__ __forceinline__ void stream_consume(StreamBars& s, const StreamParams& p, int r0, int r1, int tiles, DevStatus* status, Of of) {
+  const int q = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31, at = q * 32 + lane;   // tensor-memory lanes 32 q and on are this warp's
+  auto row_of = [&](int t) { const int r = r0 + t * p.rows + at; return t < tiles && at < p.rows && r < r1 ? r : -1; };
+  auto scale_of = [&](int r) { return r >= 0 ? __ldg(p.b_scale + r) : 0.f; };
+  constexpr int kAhead = 4;
+  float b[kAhead];
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u) b[u] = scale_of(row_of(u));
+  bool ok = true;
+  for (int t0 = 0; t0 < tiles && ok; t0 += kAhead) {
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int t = t0 + u;
+      if (t >= tiles) break;
+      const uint32_t a = u & 1u;
+      if (!mbar_wait_bounded(smem_u32(&s.acc_full[a]), (t >> 1) & 1u, &s.abort_flag)) {
+        latch_status(status, kStatusTimeout, (5 << 28) | (blockIdx.x << 8) | a);
+        ok = false;
+      }
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      tc_fence_after();
+      of(row_of(t), b[u], s.tmem_base + a * N + (uint32_t(q * 32) << 16));
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&s.acc_empty[a]));
+      b[u] = scale_of(row_of(t + kAhead));
+    }
+  }
+}
+
+template <int N, int OUT, bool OWN = false>
+__global__ void __launch_bounds__(kStreamThreads + (OWN ? 32 * kStreamOwnWarps : 0), 1)
+int8_stream_kernel(const __grid_constant__ CUtensorMap tmTokens, const __grid_constant__ CUtensorMap tmRows, const StreamParams p, DevStatus* status) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) StreamBars bars;
+  __shared__ float a_s[4][N];   // a copy per warp; OWN: the first
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t tokens = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t ring = tokens + (uint32_t)p.k_blocks * N * 128u;
+  stream_begin<N>(bars, OWN ? &tmRows : &tmTokens, &tmRows, 4, OWN ? 4 + kStreamOwnWarps : 1);
   const int r0 = (int)((long long)p.V * blockIdx.x / gridDim.x), r1 = (int)((long long)p.V * (blockIdx.x + 1) / gridDim.x);
   const int tiles = (r1 - r0 + p.rows - 1) / p.rows;
 
   if (warp == 0) {
-    if (lane == 0) {
-      const uint32_t tok_bar = smem_u32(&bar_tokens);
-      if (!OWN) mbar_arrive_expect_tx(tok_bar, (uint32_t)p.k_blocks * N * 128u);
-      for (int kb = 0; !OWN && kb < p.k_blocks; ++kb) tma_load_2d(tokens + (uint32_t)kb * N * 128u, &tmTokens, tok_bar, kb * 128, 0);
-      int stage = 0;
-      uint32_t phase = 0;
-      bool ok = true;
-      for (int t = 0; t < tiles && ok; ++t) {
-        for (int kb = 0; kb < p.k_blocks; ++kb) {
-          if (!mbar_wait_bounded(smem_u32(&bar_empty[stage]), phase ^ 1u, abort_p)) {
-            latch_status(status, kStatusTimeout, (1 << 28) | (blockIdx.x << 8) | stage);
-            ok = false;
-            break;
-          }
-          const uint32_t full = smem_u32(&bar_full[stage]);
-          mbar_arrive_expect_tx(full, (uint32_t)p.rows * 128u);
-          tma_load_2d(ring + (uint32_t)stage * kStreamStageBytes, &tmRows, full, kb * 128, r0 + t * p.rows);
-          if (++stage == p.stages) { stage = 0; phase ^= 1u; }
-        }
-      }
-      if (!ok) {
-        // copies already issued land before the block's shared memory goes away
-        for (int s = 0; s < p.stages; ++s) {
-          const uint32_t ph = s < stage ? phase : (phase ^ 1u);
-          for (int it = 0; it < 4096 && !mbar_try_wait(smem_u32(&bar_full[s]), ph); ++it) {}
-        }
-        for (int it = 0; !OWN && it < 4096 && !mbar_try_wait(tok_bar, 0); ++it) {}
-      }
-    }
+    if (lane == 0) stream_produce<N>(bars, OWN ? nullptr : &tmTokens, &tmRows, p, tokens, ring, r0, tiles, status);
   } else if (warp == 1) {
-    if (lane == 0) {
-      constexpr uint32_t idesc = make_idesc_s8(128, N);
-      constexpr uint64_t hi = make_smem_desc_hi(16, 1024);
-      constexpr uint32_t hi32 = uint32_t(hi >> 32), lo_const = uint32_t(hi);
-      const uint32_t ring_lo = (ring & 0x3FFFFu) >> 4, tok_lo = (tokens & 0x3FFFFu) >> 4;
-      int stage = 0;
-      uint32_t phase = 0;
-      bool ok = tiles == 0 || mbar_wait_bounded(smem_u32(&bar_tokens), 0, abort_p);
-      if (!ok) latch_status(status, kStatusTimeout, (3 << 28) | (blockIdx.x << 8) | 0xff);
-      for (int t = 0; t < tiles && ok; ++t) {
-        const uint32_t a = t & 1u;
-        if (!mbar_wait_bounded(smem_u32(&bar_acc_empty[a]), ((t >> 1) & 1u) ^ 1u, abort_p)) {
-          latch_status(status, kStatusTimeout, (2 << 28) | (blockIdx.x << 8) | a);
-          ok = false;
-          break;
-        }
-        tc_fence_after();
-        for (int kb = 0; kb < p.k_blocks; ++kb) {
-          if (!mbar_wait_bounded(smem_u32(&bar_full[stage]), phase, abort_p)) {
-            latch_status(status, kStatusTimeout, (3 << 28) | (blockIdx.x << 8) | stage);
-            ok = false;
-            break;
-          }
-          tc_fence_after();
-          const uint32_t w = lo_const | (ring_lo + (uint32_t)stage * (kStreamStageBytes >> 4)), x = lo_const | (tok_lo + (uint32_t)kb * (N * 128 >> 4));
-#pragma unroll
-          for (int k = 0; k < 4; ++k) umma_i8_words<1>(tmem_base + a * N, w + 2 * k, hi32, x + 2 * k, hi32, idesc, (kb > 0 || k > 0) ? 1u : 0u);
-          umma_commit(smem_u32(&bar_empty[stage]));
-          if (++stage == p.stages) { stage = 0; phase ^= 1u; }
-        }
-        if (ok) umma_commit(smem_u32(&bar_acc_full[a]));
-      }
-      umma_commit(smem_u32(&bar_drain));
-      bool drained = false;
-      for (int it = 0; it < (1 << 22) && !drained; ++it) drained = mbar_try_wait(smem_u32(&bar_drain), 0) != 0;
-      if (!drained) latch_status(status, kStatusTimeout, (4 << 28) | (blockIdx.x << 8));
-    }
+    if (lane == 0) stream_multiply<N>(bars, p, tokens, ring, tiles, status);
   } else {
-    const int q = warp & 3, at = q * 32 + lane;   // tensor-memory lanes 32 q and on are this warp's
-    float* scales = a_s[OWN ? 0 : q];
+    float* scales = a_s[OWN ? 0 : warp & 3];
     bool ok = true;
     if constexpr (OWN) {
       // rows of the swizzled operand: 128 bytes of a k-block, 16-byte chunk j of row t at position j ^ (t & 7).  What lies behind the
@@ -497,38 +558,18 @@ int8_stream_kernel(const __grid_constant__ CUtensorMap tmTokens, const __grid_co
       }
       fence_proxy_async_smem();
       __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&bar_tokens));
+      if (lane == 0) mbar_arrive(smem_u32(&bars.tokens));
       if (warp < 6) {
-        ok = mbar_wait_bounded(smem_u32(&bar_tokens), 0, abort_p);   // every lane: the scales are then visible to it
+        ok = mbar_wait_bounded(smem_u32(&bars.tokens), 0, &bars.abort_flag);   // every lane: the scales are then visible to it
         ok = __all_sync(0xffffffffu, ok);
       }
     } else {
       for (int t = lane; t < N; t += 32) scales[t] = t < p.T ? p.a_scale[t] : 0.f;
       __syncwarp();
     }
-    const int my_tiles = warp < 6 ? tiles : 0;
-    auto row_of = [&](int t) { const int r = r0 + t * p.rows + at; return t < my_tiles && at < p.rows && r < r1 ? r : -1; };
-    auto scale_of = [&](int r) { return r >= 0 ? __ldg(p.b_scale + r) : 0.f; };
-    // scales of this thread's rows, kAhead tiles early: while the ring streams B such a load takes as long as a tile or two
-    constexpr int kAhead = 4;
-    float b[kAhead];
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) b[u] = scale_of(row_of(u));
-    for (int t0 = 0; t0 < my_tiles && ok; t0 += kAhead) {
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        const int t = t0 + u, r = row_of(t);
-        if (t >= my_tiles) break;
-        const uint32_t a = u & 1u;
-        if (!mbar_wait_bounded(smem_u32(&bar_acc_full[a]), (t >> 1) & 1u, abort_p)) {
-          latch_status(status, kStatusTimeout, (5 << 28) | (blockIdx.x << 8) | a);
-          ok = false;
-        }
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
-        tc_fence_after();
-        const uint32_t taddr = tmem_base + a * N + (uint32_t(q * 32) << 16);
-        size_t out = r >= 0 ? (size_t)r : 0;
+    if (warp < 6 && ok) {
+      stream_consume<N>(bars, p, r0, r1, tiles, status, [&](int r, float b, uint32_t taddr) {
+        const size_t out = r >= 0 ? (size_t)r : 0;
         constexpr int kStep = N % 32 ? 16 : 32;
 #pragma unroll 1
         for (int c = 0; c < N; c += kStep) {
@@ -540,24 +581,106 @@ int8_stream_kernel(const __grid_constant__ CUtensorMap tmTokens, const __grid_co
           if (r >= 0) {
 #pragma unroll
             for (int i = 0; i < kStep; ++i)
-              if (c + i < p.T) store_one<OUT>(p.C, out + (size_t)(c + i) * p.ldC, (float)(int)x[i] * scales[c + i] * b[u]);
+              if (c + i < p.T) store_one<OUT>(p.C, out + (size_t)(c + i) * p.ldC, (float)(int)x[i] * scales[c + i] * b);
           }
         }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&bar_acc_empty[a]));
-        b[u] = scale_of(row_of(t + kAhead));
-      }
+      });
     }
   }
-  chain_release();
-  tc_fence_before();
-  __syncthreads();
-  if (warp == 1) {
-    __syncwarp();
-    tc_fence_after();
-    tmem_dealloc(tmem_base, kCols);
+  stream_end<N>(bars);
+}
+
+// Statistics of RowStats over the same logits: scoring of up to N tokens.  Eight warps, two per 32 rows of B with half of the tokens
+// each; a thread keeps maximum, sum and weighted sum of every token over its own rows of all tiles, so that a logit costs one
+// exponential and no exchange; the threads' numbers are merged once, at the end, in a fixed order.  One float4 per (block, token).
+constexpr int kStreamStatsThreads = 64 + 8 * 32;
+template <int N>
+__global__ void __launch_bounds__(kStreamStatsThreads, 1)
+int8_stream_stats_kernel(const __grid_constant__ CUtensorMap tmTokens, const __grid_constant__ CUtensorMap tmRows, const StreamParams p,
+                         const int* tokens_c, float4* partials, int part_stride, DevStatus* status) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) StreamBars bars;
+  constexpr int kMine = N / 2;
+  __shared__ float a_s[N], zy_s[N];
+  __shared__ int y_s[N];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t tokens = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t ring = tokens + (uint32_t)p.k_blocks * N * 128u;
+  // [4][N] in the tokens' place: a warp that is through its last tile knows that every product has read them
+  float4* part_s = reinterpret_cast<float4*>(smem_raw + (tokens - smem_u32(smem_raw)));
+  static_assert(4 * sizeof(float4) <= 128, "four per token, where a token has 128 bytes at least");
+  stream_begin<N>(bars, &tmTokens, &tmRows, 8, 1);
+  const int n = min(status->n_valid, N);
+  const int r0 = (int)((long long)p.V * blockIdx.x / gridDim.x), r1 = (int)((long long)p.V * (blockIdx.x + 1) / gridDim.x);
+  const int tiles = n > 0 ? (r1 - r0 + p.rows - 1) / p.rows : 0;
+  if (blockIdx.x == 0 && threadIdx.x == 0) status->n_ranges = gridDim.x;
+  for (int t = threadIdx.x; t < N; t += kStreamStatsThreads) {
+    a_s[t] = t < n ? p.a_scale[t] : 0.f;
+    y_s[t] = t < n ? tokens_c[t] : -1;
+    zy_s[t] = 0.f;
   }
+  __syncthreads();
+
+  if (warp == 0) {
+    if (lane == 0 && tiles > 0) stream_produce<N>(bars, &tmTokens, &tmRows, p, tokens, ring, r0, tiles, status);
+  } else if (warp == 1) {
+    if (lane == 0) stream_multiply<N>(bars, p, tokens, ring, tiles, status);
+  } else {
+    const int first = (warp - 2) / 4 * kMine;   // first of this warp's tokens
+    float m[kMine], s[kMine], a[kMine];
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) { m[i] = -CUDART_INF_F; s[i] = a[i] = 0.f; }
+    stream_consume<N>(bars, p, r0, r1, tiles, status, [&](int r, float b, uint32_t taddr) {
+#pragma unroll
+      for (int c = 0; c < kMine; c += 8) {
+        uint32_t x[8];
+        tmem_ld_32x8(taddr + first + c, x);
+        tmem_ld_wait();
+        if (r >= 0) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int t = c + i;
+            const float z = (float)(int)x[i] * a_s[first + t] * b;
+            if (r == y_s[first + t]) zy_s[first + t] = z;
+            // the smaller of the two exponents is 0
+            const float d = z - m[t], e = ex2_approx(-fabsf(d) * kLog2e);
+            const bool up = d > 0.f;
+            s[t] = up ? fmaf(s[t], e, 1.f) : s[t] + e;
+            a[t] = up ? fmaf(a[t], e, z) : fmaf(e, z, a[t]);
+            m[t] = fmaxf(m[t], z);
+          }
+        }
+      }
+    });
+    // over the warp's rows; a thread without a row has m = -inf and sums of 0
+#pragma unroll
+    for (int t = 0; t < kMine; ++t) {
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) {
+        const float m2 = __shfl_xor_sync(0xffffffffu, m[t], o), s2 = __shfl_xor_sync(0xffffffffu, s[t], o), a2 = __shfl_xor_sync(0xffffffffu, a[t], o);
+        const float mx = fmaxf(m[t], m2);
+        const float f = m[t] == mx ? 1.f : ex2_approx((m[t] - mx) * kLog2e), f2 = m2 == mx ? 1.f : ex2_approx((m2 - mx) * kLog2e);
+        s[t] = s[t] * f + s2 * f2;
+        a[t] = a[t] * f + a2 * f2;
+        m[t] = mx;
+      }
+      if (lane == 0) part_s[(warp & 3) * N + first + t] = make_float4(m[t], s[t], a[t], 0.f);
+    }
+  }
+  __syncthreads();
+  for (int t = threadIdx.x; t < n; t += kStreamStatsThreads) {
+    float4 x = part_s[t];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) {
+      const float4 y = part_s[w * N + t];
+      const float mx = fmaxf(x.x, y.x);
+      const float f = x.x == mx ? 1.f : ex2_approx((x.x - mx) * kLog2e), f2 = y.x == mx ? 1.f : ex2_approx((y.x - mx) * kLog2e);
+      x = make_float4(mx, x.y * f + y.y * f2, x.z * f + y.z * f2, 0.f);
+    }
+    x.w = zy_s[t];
+    partials[(size_t)blockIdx.x * part_stride + t] = x;
+  }
+  stream_end<N>(bars);
 }
 
 }  // namespace rlh

@@ -425,6 +425,7 @@ cudaError_t set_smem_attr_int8() {
     stream(int8_stream_kernel<N, kOutBf16>);
     stream(int8_stream_kernel<N, kOutF32>);
     stream(int8_stream_kernel<N, kOutF16>);
+    stream(int8_stream_stats_kernel<N>);
   };
   stream(int8_stream_kernel<kStreamOwn, kOutBf16, true>);
   stream(int8_stream_kernel<kStreamOwn, kOutF32, true>);
@@ -643,6 +644,24 @@ void launch_mask_scan(rl_ctx* c, const uint8_t* mask, int64_t T, int* block_coun
   c->launches += sums ? 2 : 3;
 }
 
+// Few tokens: the N side of the stream's tiles, and whether they fit beside a ring.
+inline int stream_tokens(int64_t T) { return T <= 16 ? 16 : T <= 32 ? 32 : T <= 48 ? 48 : 64; }
+inline bool streams(int64_t T, int64_t d) { return T <= 64 && stream_stages(stream_tokens(T), (int)((d + 127) / 128)) >= kStreamMinStages; }
+
+// Shape of a stream of B on at most `most` blocks; the blocks.
+inline int stream_shape(StreamParams& p, const float* b_scale, int64_t T, int64_t d, int64_t V, int most) {
+  p.b_scale = b_scale;
+  p.T = (int)T;
+  p.V = (int)V;
+  p.d = (int)d;
+  p.k_blocks = (int)((d + 127) / 128);
+  p.stages = stream_stages(stream_tokens(T), p.k_blocks);
+  const int blocks = (int)(V < most ? V : most);
+  const int64_t per = (V + blocks - 1) / blocks, tiles = (per + 127) / 128;
+  p.rows = (int)((per + tiles - 1) / tiles);
+  return blocks;
+}
+
 // Which part of the forward stage a call needs, and where its rows of W sit in the vocabulary.
 struct FwdPlan {
   bool scan = true;          // mask scan (false: the row map of an earlier call on this workspace is reused)
@@ -685,6 +704,8 @@ rl_status run_forward(rl_ctx* c, const WsLayout& L, const void* H, int64_t ldH, 
   pp.ticket = reinterpret_cast<unsigned*>(reinterpret_cast<char*>(c->dstatus) + kTicketOffset);
   pp.H_scale = plan.H_scale;
   pp.scale_c = int8_row_scales(L, ws, d);
+  const bool stream = plan.W_scale && streams(T, d);
+  pp.unpadded = stream;
   auto prep = [&](int blocks, auto copy, auto stored, auto to_int8) {
     launch(c, plan.W_scale ? to_int8 : plan.H_scale ? stored : copy, blocks, 256, pp, c->dstatus);
   };
@@ -716,6 +737,26 @@ rl_status run_forward(rl_ctx* c, const WsLayout& L, const void* H, int64_t ldH, 
   }
   const int cg = kl ? c->cta_group : fwd_cta_group(c, L);
   CUtensorMap tmA, tmB;
+  if (stream) {
+    // few rows: W streams past all of them; a range of columns per block
+    StreamParams p = {};
+    p.a_scale = pp.scale_c;
+    const int n = stream_tokens(T), blocks = stream_shape(p, plan.W_scale, T, d, V, c->grid[1] < L.part_ranges ? c->grid[1] : L.part_ranges);
+    if (!map_kmajor_i8(c, &tmA, Hc, (uint64_t)L.Tpad, (uint64_t)d, (uint64_t)d, (uint32_t)n) ||
+        !map_kmajor_i8(c, &tmB, W, (uint64_t)V, (uint64_t)d, (uint64_t)ldW, (uint32_t)p.rows))
+      return RL_ERR_CUDA;
+    const int pr = prof_begin(c, 0);
+    auto go = [&](auto kernel) {
+      launch_smem(c, kernel, blocks, kStreamStatsThreads, kStreamSmem, tmA, tmB, p, tokens_c, reinterpret_cast<float4*>(ws + L.partials), L.Tpad, c->dstatus);
+    };
+    if (n == 16) go(int8_stream_stats_kernel<16>);
+    else if (n == 32) go(int8_stream_stats_kernel<32>);
+    else if (n == 48) go(int8_stream_stats_kernel<48>);
+    else go(int8_stream_stats_kernel<64>);
+    prof_end(c, pr, 0);
+    c->launches++;
+    return cuda_ok();
+  }
   auto map_k = plan.W_scale ? map_kmajor_i8 : map_kmajor;
   if (!map_k(c, &tmA, Hc, (uint64_t)L.Tpad, (uint64_t)d, (uint64_t)d, BM)) return RL_ERR_CUDA;
   if (!map_k(c, &tmB, W, (uint64_t)V, (uint64_t)d, (uint64_t)ldW, b_box_rows(cg))) return RL_ERR_CUDA;
@@ -1873,25 +1914,12 @@ static rl_status check_int8(const void* B, int64_t ldB, const float* b_scale, in
   return RL_OK;
 }
 
-// Few tokens: the N side of the stream's tiles, and whether they fit beside a ring.
-static inline int stream_tokens(int64_t T) { return T <= 16 ? 16 : T <= 32 ? 32 : T <= 48 ? 48 : 64; }
-static inline bool streams(int64_t T, int64_t d) { return T <= 64 && stream_stages(stream_tokens(T), (int)((d + 127) / 128)) >= kStreamMinStages; }
-
 // tokens == NULL: p.X has them in bf16.
 static rl_status int8_stream(rl_ctx* c, const CUtensorMap* tokens, StreamParams p, const int8_t* B, int64_t ldB, const float* b_scale,
                              int64_t T, int64_t d, int64_t V, void* C, int c_dtype, int64_t ldC) {
-  const int n = stream_tokens(T);
-  p.b_scale = b_scale;
-  p.T = (int)T;
-  p.V = (int)V;
-  p.d = (int)d;
-  p.k_blocks = (int)((d + 127) / 128);
-  p.stages = stream_stages(n, p.k_blocks);
+  const int n = stream_tokens(T), blocks = stream_shape(p, b_scale, T, d, V, c->grid[1]);
   p.C = C;
   p.ldC = ldC;
-  const int64_t per = (V + c->grid[1] - 1) / c->grid[1], tiles = (per + 127) / 128;
-  p.rows = (int)((per + tiles - 1) / tiles);
-  const int blocks = (int)(V < c->grid[1] ? V : c->grid[1]);
   CUtensorMap w;
   if (!map_kmajor_i8(c, &w, B, (uint64_t)V, (uint64_t)d, (uint64_t)ldB, (uint32_t)p.rows)) return RL_ERR_CUDA;
   const int pr = prof_begin(c, 0);

@@ -186,6 +186,7 @@ struct PrepParams {
   unsigned* ticket;       // of the loss kernels that follow: cleared, whatever became of the call before
   const float* H_scale;   // kRowsStored: of every row of H, which then points to 8-bit integers
   float* scale_c;         // kRowsToInt8: of the compact rows, which then are 8-bit integers
+  int unpadded;           // kRowsToInt8: no rows of zeros behind them (int8_stream_stats_kernel does without)
 };
 // How rows become compact: as they are; from rows stored in 8 bits (int8_head.cuh) to the bf16 that those stand for; or from bf16 to 8 bits.
 enum RowKind { kRowsCopy = 0, kRowsStored = 1, kRowsToInt8 = 2 };
@@ -269,7 +270,7 @@ __global__ void __launch_bounds__(256) prep_rows_kernel(const PrepParams p, DevS
     n = st->n_valid;
     for (int t = blockIdx.x * warps + warp; t < p.T; t += gridDim.x * warps) prep_row<KIND>(p, t, p.row_pos[t], lane, st);
   }
-  const int n_pad = (n + 127) / 128 * 128;
+  const int n_pad = KIND == kRowsToInt8 && p.unpadded ? n : (n + 127) / 128 * 128;
   for (int i = n + blockIdx.x * warps + warp; i < n_pad; i += gridDim.x * warps) {
     constexpr int kBytes = KIND == kRowsToInt8 ? 1 : 2;
     uint4* dst = reinterpret_cast<uint4*>(reinterpret_cast<char*>(p.Hc) + (size_t)i * p.d * kBytes);

@@ -293,7 +293,9 @@ def test_two_contexts_at_once():
 
 
 # ------------------------------------------------------------------ scoring
-@pytest.mark.parametrize("T,d,V", [(1, 64, 1), (1, 64, 300), (77, 192, 1000), (128, 2048, 3000), (129, 1024, 777), (700, 2176, 1500), (2000, 256, 5000)])
+@pytest.mark.parametrize("T,d,V", [(1, 64, 1), (1, 64, 300), (77, 192, 1000), (128, 2048, 3000), (129, 1024, 777), (700, 2176, 1500), (2000, 256, 5000),
+                                   (2, 128, 2), (16, 2048, 50000), (17, 3584, 3001), (40, 256, 151), (48, 1024, 20000), (64, 2048, 4099), (64, 64, 40000),
+                                   (64, 2560, 3000), (33, 64, 17)])
 def test_scoring(ctx, T, d, V):
     g = torch.Generator(DEV).manual_seed(T + d)
     W = _rows(V, d, torch.bfloat16, seed=1, std=0.05)
@@ -323,9 +325,9 @@ def test_scoring(ctx, T, d, V):
         assert bool((x[~on] == 0).all())
 
 
-@pytest.mark.parametrize("T", [100, 300])
+@pytest.mark.parametrize("T", [1, 20, 64, 100, 300])
 def test_scoring_nothing_that_counts(ctx, T):
-    """No valid row, before and after calls that have some: what a pass has fetched ahead is dropped."""
+    """No valid row, or one, before and after calls that have more."""
     W = _rows(3000, 448, torch.bfloat16, seed=1, std=0.05)
     H = _rows(T, 448, torch.bfloat16, seed=2)
     tok = torch.randint(0, 3000, (T,), device=DEV, dtype=torch.int32)
