@@ -32,17 +32,53 @@ __device__ __forceinline__ uint32_t pack4(const RowScale& c, float x0, float x1,
   const uint32_t w = __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(d, e, 0x0040), 0x5410);
   return c.r == 0.f ? 0u : w;
 }
-__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
-// Eight bf16 values to eight bytes.
-__device__ __forceinline__ uint2 pack8_bf16(const RowScale& c, const uint4& v) {
-  return make_uint2(pack4(c, bf16_lo(v.x), bf16_hi(v.x), bf16_lo(v.y), bf16_hi(v.y)),
-                    pack4(c, bf16_lo(v.z), bf16_hi(v.z), bf16_lo(v.w), bf16_hi(v.w)));
-}
-__device__ __forceinline__ uint32_t most_bf16(const uint4& v) {   // two maxima, as 16-bit words
-  constexpr uint32_t k = 0x7fff7fffu;
-  return __vmaxu2(__vmaxu2(v.x & k, v.y & k), __vmaxu2(v.z & k, v.w & k));
-}
+// Eight elements of a row as they were loaded: the running maximum of their magnitudes (two 16-bit words, or the bits of a float),
+// the bits of the float that it is, and the eight bytes that they become.
+template <class T>
+struct Eight;
+template <>
+struct Eight<__nv_bfloat16> {
+  uint4 v;
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) { v = __ldg(reinterpret_cast<const uint4*>(p)); }
+  __device__ __forceinline__ uint32_t most(uint32_t m) const {
+    constexpr uint32_t k = 0x7fff7fffu;
+    return __vmaxu2(m, __vmaxu2(__vmaxu2(v.x & k, v.y & k), __vmaxu2(v.z & k, v.w & k)));
+  }
+  __device__ static __forceinline__ uint32_t larger(uint32_t m) { return max(m & 0xffffu, m >> 16); }
+  __device__ static __forceinline__ uint32_t bits(uint32_t m) { return m << 16; }
+  __device__ __forceinline__ uint2 pack(const RowScale& c) const {
+    auto lo = [](uint32_t w) { return __uint_as_float(w << 16); };
+    auto hi = [](uint32_t w) { return __uint_as_float(w & 0xffff0000u); };
+    return make_uint2(pack4(c, lo(v.x), hi(v.x), lo(v.y), hi(v.y)), pack4(c, lo(v.z), hi(v.z), lo(v.w), hi(v.w)));
+  }
+};
+template <>
+struct Eight<__half> : Eight<__nv_bfloat16> {
+  __device__ __forceinline__ void load(const __half* p) { v = __ldg(reinterpret_cast<const uint4*>(p)); }
+  __device__ static __forceinline__ uint32_t bits(uint32_t m) { return __float_as_uint(__half2float(__ushort_as_half((unsigned short)m))); }
+  __device__ __forceinline__ uint2 pack(const RowScale& c) const {
+    auto of = [](uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); };
+    const float2 a = of(v.x), b = of(v.y), d = of(v.z), e = of(v.w);
+    return make_uint2(pack4(c, a.x, a.y, b.x, b.y), pack4(c, d.x, d.y, e.x, e.y));
+  }
+};
+template <>
+struct Eight<float> {
+  float4 a, b;
+  __device__ __forceinline__ void load(const float* p) {
+    a = __ldg(reinterpret_cast<const float4*>(p));
+    b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+  }
+  __device__ __forceinline__ uint32_t most(uint32_t m) const {
+    auto u = [](float x) { return __float_as_uint(x) & 0x7fffffffu; };
+    return max(m, max(max(max(u(a.x), u(a.y)), max(u(a.z), u(a.w))), max(max(u(b.x), u(b.y)), max(u(b.z), u(b.w)))));
+  }
+  __device__ static __forceinline__ uint32_t larger(uint32_t m) { return m; }
+  __device__ static __forceinline__ uint32_t bits(uint32_t m) { return m; }
+  __device__ __forceinline__ uint2 pack(const RowScale& c) const {
+    return make_uint2(pack4(c, a.x, a.y, a.z, a.w), pack4(c, b.x, b.y, b.z, b.w));
+  }
+};
 __device__ __forceinline__ uint32_t warp_max(uint32_t v) { return __reduce_max_sync(0xffffffffu, v); }
 // What is stored in 8 bits, as the bf16 that the products of the loss take: 16 bytes to 16 values.
 __device__ __forceinline__ void unpack16(const uint4& q, float s, uint4& lo, uint4& hi) {
@@ -54,51 +90,40 @@ __device__ __forceinline__ void unpack16(const uint4& q, float s, uint4& lo, uin
   lo = make_uint4(two(q.x, 0), two(q.x, 2), two(q.y, 0), two(q.y, 2));
   hi = make_uint4(two(q.z, 0), two(q.z, 2), two(q.w, 0), two(q.w, 2));
 }
-// One bf16 row of 8 * vecs elements, 16-byte aligned, by one warp: put(v, bytes of elements 8 v to 8 v + 7); the scale.  What does not fit
-// HELD words per lane is read twice.
-template <int HELD, class Put>
-__device__ __forceinline__ float quantize_row_bf16(const uint4* src, int vecs, int lane, Put put) {
-  uint4 h[HELD];
-  uint32_t m2 = 0;
-#pragma unroll
-  for (int i = 0; i < HELD; ++i) {
-    h[i] = lane + 32 * i < vecs ? __ldg(src + lane + 32 * i) : make_uint4(0, 0, 0, 0);
-    m2 = __vmaxu2(m2, most_bf16(h[i]));
-  }
-  for (int v = lane + 32 * HELD; v < vecs; v += 32) m2 = __vmaxu2(m2, most_bf16(__ldg(src + v)));
-  const RowScale c = row_scale(warp_max(max(m2 & 0xffffu, m2 >> 16)) << 16);
+// One row of 8 * vecs elements, 16-byte aligned, by one warp: put(v, bytes of elements 8 v to 8 v + 7); the scale.  What does not fit
+// HELD loads per lane is read twice.
+template <int HELD, class T, class Put>
+__device__ __forceinline__ float quantize_row(const T* src, int vecs, int lane, Put put) {
+  Eight<T> h[HELD];
+  uint32_t m = 0;
 #pragma unroll
   for (int i = 0; i < HELD; ++i)
-    if (lane + 32 * i < vecs) put(lane + 32 * i, pack8_bf16(c, h[i]));
-  for (int v = lane + 32 * HELD; v < vecs; v += 32) put(v, pack8_bf16(c, __ldg(src + v)));
+    if (lane + 32 * i < vecs) h[i].load(src + (lane + 32 * i) * 8);
+#pragma unroll
+  for (int i = 0; i < HELD; ++i)
+    if (lane + 32 * i < vecs) m = h[i].most(m);
+  for (int v = lane + 32 * HELD; v < vecs; v += 32) {
+    Eight<T> x;
+    x.load(src + v * 8);
+    m = x.most(m);
+  }
+  const RowScale c = row_scale(Eight<T>::bits(warp_max(Eight<T>::larger(m))));
+#pragma unroll
+  for (int i = 0; i < HELD; ++i)
+    if (lane + 32 * i < vecs) put(lane + 32 * i, h[i].pack(c));
+  for (int v = lane + 32 * HELD; v < vecs; v += 32) {
+    Eight<T> x;
+    x.load(src + v * 8);
+    put(v, x.pack(c));
+  }
   return c.s;
 }
 
-// Any rows: a warp per row, eight elements per lane and step.  VEC: rows start on 16 bytes; else, and at a row's ragged end, one
-// element after the other.
-template <class T>
-__device__ __forceinline__ float as_float(T x) {
-  if constexpr (sizeof(T) == 4) return x;
-  else return (float)x;
-}
-template <class T, bool VEC>
-__device__ __forceinline__ void load8(const T* row, int64_t k, int64_t d, float (&x)[8]) {
-  if (VEC && k + 8 <= d) {
-    if constexpr (sizeof(T) == 4) {
-      const float4 a = __ldg(reinterpret_cast<const float4*>(row + k)), b = __ldg(reinterpret_cast<const float4*>(row + k) + 1);
-      x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-    } else {
-      const uint4 v = __ldg(reinterpret_cast<const uint4*>(row + k));
-      const T* e = reinterpret_cast<const T*>(&v);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = as_float(e[i]);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = k + i < d ? as_float(row[k + i]) : 0.f;
-  }
-}
-template <class T, bool VEC>
+// Any rows, a warp each.  HELD > 0: 16-byte aligned rows of a multiple of 8 elements, quantize_row<HELD>; else one element after the other.
+// As many loads per lane as a row has, no more: bf16, 65536 rows of 896 elements 29.8 us with 4, 37.6 with 8, 60.9 with 16; of 3584 118 with 8, 113
+// with 16 (6.2 TB/s).  151936 rows of 2048: bf16 135 us, fp16 135, fp32 217 (6.9-7.2 TB/s; read twice, in fp16 214 and in fp32 331).  Rows
+// of 999: fp16 2.8, fp32 3.8 TB/s.
+template <class T, int HELD>
 __global__ void __launch_bounds__(256) quantize_rows_kernel(const T* X, int64_t ldX, int64_t rows, int64_t d, int8_t* Q, int64_t ldQ,
                                                             float* scale) {
   chain_begin();
@@ -106,32 +131,17 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const T* X, int64_t 
   for (int64_t r = (int64_t)blockIdx.x * warps + (threadIdx.x >> 5); r < rows; r += (int64_t)gridDim.x * warps) {
     const T* src = X + r * ldX;
     int8_t* dst = Q + r * ldQ;
-    if constexpr (VEC && std::is_same<T, __nv_bfloat16>::value) {
-      if (d % 8 == 0) {
-        const float s = quantize_row_bf16<8>(reinterpret_cast<const uint4*>(src), (int)(d / 8), lane, [&](int v, uint2 w) { reinterpret_cast<uint2*>(dst)[v] = w; });
-        if (lane == 0) scale[r] = s;
-        continue;
-      }
+    float s;
+    if constexpr (HELD > 0) {
+      s = quantize_row<HELD>(src, (int)(d / 8), lane, [&](int v, uint2 w) { reinterpret_cast<uint2*>(dst)[v] = w; });
+    } else {
+      uint32_t m = 0;
+      for (int64_t k = lane; k < d; k += 32) m = max(m, __float_as_uint((float)src[k]) & 0x7fffffffu);
+      const RowScale c = row_scale(warp_max(m));
+      for (int64_t k = lane; k < d; k += 32) dst[k] = (int8_t)pack4(c, (float)src[k], 0.f, 0.f, 0.f);   // what lies behind the row stays
+      s = c.s;
     }
-    uint32_t m = 0;
-    for (int64_t k = lane * 8; k < d; k += 256) {
-      float x[8];
-      load8<T, VEC>(src, k, d, x);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
-    }
-    const RowScale c = row_scale(warp_max(m));
-    for (int64_t k = lane * 8; k < d; k += 256) {
-      float x[8];
-      load8<T, VEC>(src, k, d, x);
-      const uint2 w = make_uint2(pack4(c, x[0], x[1], x[2], x[3]), pack4(c, x[4], x[5], x[6], x[7]));
-      if (k + 8 <= d) {
-        *reinterpret_cast<uint2*>(dst + k) = w;
-      } else {
-        for (int i = 0; k + i < d; ++i) dst[k + i] = (int8_t)((i < 4 ? w.x : w.y) >> (8 * (i & 3)));   // what lies behind the row stays
-      }
-    }
-    if (lane == 0) scale[r] = c.s;
+    if (lane == 0) scale[r] = s;
   }
 }
 
@@ -550,7 +560,7 @@ int8_stream_kernel(const __grid_constant__ CUtensorMap tmTokens, const __grid_co
       // rows of the swizzled operand: 128 bytes of a k-block, 16-byte chunk j of row t at position j ^ (t & 7).  What lies behind the
       // tokens, and behind d (where B reads as zeros), may hold anything
       for (int t = warp - 2; t < p.T; t += 4 + kStreamOwnWarps) {
-        const float sc = quantize_row_bf16<16>(reinterpret_cast<const uint4*>(p.X + t * p.ldX), p.d / 8, lane, [&](int v, uint2 w) {
+        const float sc = quantize_row<16>(p.X + t * p.ldX, p.d / 8, lane, [&](int v, uint2 w) {
           const uint32_t to = tokens + (uint32_t)(v >> 4) * (N * 128u) + t * 128u + ((uint32_t(v >> 1 & 7) ^ uint32_t(t & 7)) << 4) + (v & 1) * 8u;
           asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(to), "r"(w.x), "r"(w.y) : "memory");
         });

@@ -706,8 +706,8 @@ rl_status run_forward(rl_ctx* c, const WsLayout& L, const void* H, int64_t ldH, 
   pp.scale_c = int8_row_scales(L, ws, d);
   const bool stream = plan.W_scale && streams(T, d);
   pp.unpadded = stream;
-  auto prep = [&](int blocks, auto copy, auto stored, auto to_int8) {
-    launch(c, plan.W_scale ? to_int8 : plan.H_scale ? stored : copy, blocks, 256, pp, c->dstatus);
+  auto prep = [&](int blocks, auto copy, auto stored, auto to_int8, auto to_int8_wide) {
+    launch(c, plan.W_scale ? (d > 2048 ? to_int8_wide : to_int8) : plan.H_scale ? stored : copy, blocks, 256, pp, c->dstatus);
   };
   if (T <= kPrepRows) {
     const int pr = prof_begin(c, 5);
@@ -715,14 +715,16 @@ rl_status run_forward(rl_ctx* c, const WsLayout& L, const void* H, int64_t ldH, 
     int rows = (int)align_up((size_t)(T + c->n_sm * 4 - 1) / (c->n_sm * 4), 8);
     if (rows > 256) rows = 256;
     pp.rows_per_block = rows;
-    prep((int)((T + rows - 1) / rows), prep_rows_kernel<true, kRowsCopy>, prep_rows_kernel<true, kRowsStored>, prep_rows_kernel<true, kRowsToInt8>);
+    prep((int)((T + rows - 1) / rows), prep_rows_kernel<true, kRowsCopy>, prep_rows_kernel<true, kRowsStored>, prep_rows_kernel<true, kRowsToInt8>,
+         prep_rows_kernel<true, kRowsToInt8Wide>);
     prof_end(c, pr, 5);
   } else {
     int* row_pos = reinterpret_cast<int*>(ws + L.row_pos);
     if (plan.scan) launch_mask_scan(c, mask, T, reinterpret_cast<int*>(ws + L.scan_counts), row_map, row_pos);
     pp.row_pos = row_pos;
     const int pr = prof_begin(c, 5);
-    prep(c->n_sm * 8, prep_rows_kernel<false, kRowsCopy>, prep_rows_kernel<false, kRowsStored>, prep_rows_kernel<false, kRowsToInt8>);
+    prep(c->n_sm * 8, prep_rows_kernel<false, kRowsCopy>, prep_rows_kernel<false, kRowsStored>, prep_rows_kernel<false, kRowsToInt8>,
+         prep_rows_kernel<false, kRowsToInt8Wide>);
     prof_end(c, pr, 5);
   }
   c->launches += 1;
@@ -1886,16 +1888,21 @@ rl_status rl_quantize_rows(rl_ctx* c, const void* X, int x_dtype, int64_t ldX, i
   const uintptr_t elem = x_dtype == RL_FP32 ? 4 : 2, at = reinterpret_cast<uintptr_t>(X);
   if (at % elem || (reinterpret_cast<uintptr_t>(scale) & 3) || (reinterpret_cast<uintptr_t>(Q) & 15) || ldQ % 16) return RL_ERR_ALIGNMENT;
   const OnDevice on(c);
-  const bool vec = at % 16 == 0 && ldX * elem % 16 == 0;
+  const bool vec = at % 16 == 0 && ldX * elem % 16 == 0 && d % 8 == 0;
   int64_t blocks = (rows + 7) / 8;   // a warp per row
   if (blocks > (int64_t)c->n_sm * 64) blocks = (int64_t)c->n_sm * 64;
   const int pr = prof_begin(c, 5);
-  auto rows_of = [&](auto* x, auto by_vec, auto by_one) {
-    launch(c, vec ? by_vec : by_one, (int)blocks, 256, x, ldX, rows, d, Q, ldQ, scale);
+  auto rows_of = [&](auto* x) {
+    using E = std::remove_const_t<std::remove_pointer_t<decltype(x)>>;
+    auto go = [&](auto kernel) { launch(c, kernel, (int)blocks, 256, x, ldX, rows, d, Q, ldQ, scale); };
+    if (!vec) go(quantize_rows_kernel<E, 0>);
+    else if (d <= 1024) go(quantize_rows_kernel<E, 4>);
+    else if (d <= 2048 || sizeof(E) == 4) go(quantize_rows_kernel<E, 8>);
+    else go(quantize_rows_kernel<E, 16>);
   };
-  if (x_dtype == RL_BF16) rows_of(static_cast<const __nv_bfloat16*>(X), quantize_rows_kernel<__nv_bfloat16, true>, quantize_rows_kernel<__nv_bfloat16, false>);
-  else if (x_dtype == RL_FP16) rows_of(static_cast<const __half*>(X), quantize_rows_kernel<__half, true>, quantize_rows_kernel<__half, false>);
-  else rows_of(static_cast<const float*>(X), quantize_rows_kernel<float, true>, quantize_rows_kernel<float, false>);
+  if (x_dtype == RL_BF16) rows_of(static_cast<const __nv_bfloat16*>(X));
+  else if (x_dtype == RL_FP16) rows_of(static_cast<const __half*>(X));
+  else rows_of(static_cast<const float*>(X));
   prof_end(c, pr, 5);
   c->launches++;
   return cuda_ok();

@@ -189,7 +189,10 @@ struct PrepParams {
   int unpadded;           // kRowsToInt8: no rows of zeros behind them (int8_stream_stats_kernel does without)
 };
 // How rows become compact: as they are; from rows stored in 8 bits (int8_head.cuh) to the bf16 that those stand for; or from bf16 to 8 bits.
-enum RowKind { kRowsCopy = 0, kRowsStored = 1, kRowsToInt8 = 2 };
+// (more than 2048 elements: kRowsToInt8Wide).
+enum RowKind { kRowsCopy = 0, kRowsStored = 1, kRowsToInt8 = 2, kRowsToInt8Wide = 3 };
+template <int KIND>
+constexpr bool kToInt8 = KIND >= kRowsToInt8;
 
 template <int KIND>
 __device__ __forceinline__ void prep_row(const PrepParams& p, int t, int pos, int lane, DevStatus* st) {
@@ -211,9 +214,9 @@ __device__ __forceinline__ void prep_row(const PrepParams& p, int t, int pos, in
     const float s = p.H_scale[t];
 #pragma unroll 4
     for (int v = lane; v < p.d / 16; v += 32) unpack16(__ldg(q + v), s, dst[2 * v], dst[2 * v + 1]);
-  } else if constexpr (KIND == kRowsToInt8) {
+  } else if constexpr (kToInt8<KIND>) {
     uint2* q = reinterpret_cast<uint2*>(reinterpret_cast<int8_t*>(p.Hc) + (size_t)pos * p.d);
-    const float s = quantize_row_bf16<8>(src, vec_per_row, lane, [&](int v, uint2 w) { q[v] = w; });
+    const float s = quantize_row<KIND == kRowsToInt8Wide ? 16 : 8>(p.H + (size_t)t * p.ldH, vec_per_row, lane, [&](int v, uint2 w) { q[v] = w; });
     if (lane == 0) p.scale_c[pos] = s;
   } else {
 #pragma unroll 8
@@ -270,12 +273,12 @@ __global__ void __launch_bounds__(256) prep_rows_kernel(const PrepParams p, DevS
     n = st->n_valid;
     for (int t = blockIdx.x * warps + warp; t < p.T; t += gridDim.x * warps) prep_row<KIND>(p, t, p.row_pos[t], lane, st);
   }
-  const int n_pad = KIND == kRowsToInt8 && p.unpadded ? n : (n + 127) / 128 * 128;
+  const int n_pad = kToInt8<KIND> && p.unpadded ? n : (n + 127) / 128 * 128;
   for (int i = n + blockIdx.x * warps + warp; i < n_pad; i += gridDim.x * warps) {
-    constexpr int kBytes = KIND == kRowsToInt8 ? 1 : 2;
+    constexpr int kBytes = kToInt8<KIND> ? 1 : 2;
     uint4* dst = reinterpret_cast<uint4*>(reinterpret_cast<char*>(p.Hc) + (size_t)i * p.d * kBytes);
     for (int v = lane; v < p.d * kBytes / 16; v += 32) dst[v] = make_uint4(0, 0, 0, 0);
-    if (KIND == kRowsToInt8 && lane == 0) p.scale_c[i] = 0.f;
+    if (kToInt8<KIND> && lane == 0) p.scale_c[i] = 0.f;
     if (lane == 0) p.tokens_c[i] = -1;
   }
 }

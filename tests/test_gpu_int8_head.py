@@ -30,7 +30,7 @@ def _ok(ctx):
 
 # ------------------------------------------------------------------ quantised rows
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("T,d", [(1, 1), (3, 7), (5, 16), (9, 255), (64, 1000), (33, 2048), (17, 2056), (1000, 3584), (4, 70001)])
+@pytest.mark.parametrize("T,d", [(1, 1), (3, 7), (5, 16), (9, 255), (64, 1000), (33, 2048), (17, 2056), (1000, 3584), (4, 70001), (3, 70000), (5, 4096), (2, 4104), (40, 896)])
 def test_rows_exactly(ctx, dtype, T, d):
     x = _rows(T, d, dtype, seed=T + d)
     Q, s = ctx.rl_quantize_rows(x)
