@@ -603,6 +603,9 @@ int8_stream_kernel(const __grid_constant__ CUtensorMap tmTokens, const __grid_co
 // Statistics of RowStats over the same logits: scoring of up to N tokens.  Eight warps, two per 32 rows of B with half of the tokens
 // each; a thread keeps maximum, sum and weighted sum of every token over its own rows of all tiles, so that a logit costs one
 // exponential and no exchange; the threads' numbers are merged once, at the end, in a fixed order.  One float4 per (block, token).
+// For kStreamScores tokens: a call with this / with the engine's statistics, 151936 rows, d = 256 / 1024 / 2048: 1 token 18.5 / 39.6 / 60.7 us, 30.5 /
+// 45.0 / 68.4; 32 tokens 21.1 / 38.8 / 61.4, 28.9 / 42.3 / 65.3; but 48 tokens 26.7 / 47.3 / 67.5, 28.9 / 42.0 / 65.2, and 64 slower throughout.
+constexpr int kStreamScores = 32;
 constexpr int kStreamStatsThreads = 64 + 8 * 32;
 template <int N>
 __global__ void __launch_bounds__(kStreamStatsThreads, 1)
@@ -691,6 +694,56 @@ int8_stream_stats_kernel(const __grid_constant__ CUtensorMap tmTokens, const __g
     partials[(size_t)blockIdx.x * part_stride + t] = x;
   }
   stream_end<N>(bars);
+}
+
+// Merge of a few rows' statistics, a warp per row: all its column ranges are on their way at once, in the lanes, and added up over them in
+// a fixed order.  (combine_loss_kernel, which also knows losses, takes a block per 32 rows and loads a few
+// ranges at a time.)
+struct ScoreParams {
+  const float4* partials;
+  int part_stride;
+  const int* row_map;
+  float *logp, *entropy, *lse;   // [T]; the latter two may be NULL
+};
+__global__ void __launch_bounds__(256) merge_scores_kernel(const ScoreParams p, const DevStatus* st) {
+  chain_begin();
+  const int n = st->n_valid, n_ranges = st->n_ranges, lane = threadIdx.x & 31;
+  for (int i = blockIdx.x * 8 + (threadIdx.x >> 5); i < n; i += gridDim.x * 8) {
+    const int row = p.row_map[i];
+    float M = -CUDART_INF_F, S = 0.f, A = 0.f, zy = 0.f;
+    auto add = [&](float m2, float s2, float a2) {
+      const float m = fmaxf(M, m2);
+      const float f = M == m ? 1.f : exp2f((M - m) * kLog2e), f2 = m2 == m ? 1.f : exp2f((m2 - m) * kLog2e);   // (-inf: nothing there)
+      S = S * f + s2 * f2;
+      A = A * f + a2 * f2;
+      M = m;
+    };
+    for (int r0 = 0; r0 < n_ranges; r0 += 128) {
+      float4 q[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int r = r0 + k * 32 + lane;
+        q[k] = r < n_ranges ? p.partials[(size_t)r * p.part_stride + i] : make_float4(-CUDART_INF_F, 0.f, 0.f, 0.f);
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        add(q[k].x, q[k].y, q[k].z);
+        zy += q[k].w;
+      }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      const float m2 = __shfl_xor_sync(0xffffffffu, M, o), s2 = __shfl_xor_sync(0xffffffffu, S, o), a2 = __shfl_xor_sync(0xffffffffu, A, o);
+      zy += __shfl_xor_sync(0xffffffffu, zy, o);
+      add(m2, s2, a2);
+    }
+    if (lane == 0) {
+      const float lse = M + logf(S);
+      p.logp[row] = zy - lse;
+      if (p.entropy) p.entropy[row] = lse - A / S;
+      if (p.lse) p.lse[row] = lse;
+    }
+  }
 }
 
 }  // namespace rlh
