@@ -363,21 +363,21 @@ struct EpiScale {
 // its N side.  All of the tokens lie in shared memory for the whole kernel.  (As the M side of the engine's tiles they were read again
 // for every tile by every CTA, which made the L2 slices of a few lines the bottleneck: 9 to 32 tokens took 110 to 140 us at
 // d = 3584 and 152 K rows, 40 to 128 took 97 to 101; a dp4a kernel took 95 us for one token and 139 for eight.)  Every CTA takes an equal share of the rows in tiles of `rows`.
-//   warp 0: TMA producer;  warp 1: allocates tensor memory, issues the products;  warps 2 to 5: a thread per row of B.
+//   warp 0: TMA producer;  warp 1: allocates tensor memory, issues the products;  warps 2 to 9: a thread per row of B and half of the tokens.
 constexpr int kStreamStageBytes = 128 * 128;   // 128 rows, a k-block of 128 bytes
 constexpr int kStreamMaxStages = 12, kStreamMinStages = 4;
 constexpr int kStreamSmem = 224 * 1024;        // of it 1 KB to start on a multiple of 1024
-constexpr int kStreamThreads = 192;
+constexpr int kStreamThreads = 64 + 8 * 32;
 // Stages that fit beside the tokens; fewer than kStreamMinStages: too many tokens for this kernel.
 __host__ __device__ constexpr int stream_stages(int n_tokens, int k_blocks) {
   const long long left = kStreamSmem - 1024 - (long long)n_tokens * 128 * k_blocks;
   const long long s = left < 0 ? 0 : left / kStreamStageBytes;
   return (int)(s < kStreamMaxStages ? s : kStreamMaxStages);
 }
-// Up to kStreamOwn tokens in bf16 the kernel quantises itself, in eight warps more and before these four turn to their rows, while the ring
+// Up to kStreamOwn tokens in bf16 the kernel quantises itself, in four warps more and before these eight turn to their rows, while the ring
 // fills: a launch less.  1 / 4 / 8 / 13 / 16 tokens, 151936 rows, d = 2048 52.8 / 54.3 / 55.5 / 55.8 / 56.0 us with the launch, 50.0 / 51.7 / 52.7 / 53.1 /
 // 53.6 without; d = 3584 88.0 / 90.5 / 92.4 / 93.4 / 93.5, 83.3 / 85.3 / 86.4 / 88.6 / 89.4.
-constexpr int kStreamOwn = 16, kStreamOwnWarps = 8;
+constexpr int kStreamOwn = 16, kStreamOwnWarps = 4;
 struct StreamParams {
   const __nv_bfloat16* X;   // OWN: the tokens, d a multiple of 8, rows 16-byte aligned
   long long ldX;
@@ -502,10 +502,11 @@ __device__ __forceinline__ void stream_multiply(StreamBars& s, const StreamParam
   for (int it = 0; it < (1 << 22) && !drained; ++it) drained = mbar_try_wait(smem_u32(&s.drain), 0) != 0;
   if (!drained) latch_status(status, kStatusTimeout, (4 << 28) | (blockIdx.x << 8));
 }
-// The accumulators of this block's tiles, one after the other, by one warp: of(tile u of four, row of B or -1, its scale, accumulator's address).
-// Scales of rows are loaded four tiles early: while the ring streams B such a load takes as long as a tile or two.
-template <int N, class Of>
-__device__ __forceinline__ void stream_consume(StreamBars& s, const StreamParams& p, int r0, int r1, int tiles, DevStatus* status, Of of) {
+// The accumulators of this block's tiles, one after the other, by one warp: load(accumulator's address), which is then free for the next
+// but one tile, and use(row of B or -1, its scale).  Scales of rows are loaded four tiles early: while the ring streams B such a load
+// takes as long as a tile or two.
+template <int N, class Load, class Use>
+__device__ __forceinline__ void stream_consume(StreamBars& s, const StreamParams& p, int r0, int r1, int tiles, DevStatus* status, Load load, Use use) {
   const int q = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31, at = q * 32 + lane;   // tensor-memory lanes 32 q and on are this warp's
   auto row_of = [&](int t) { const int r = r0 + t * p.rows + at; return t < tiles && at < p.rows && r < r1 ? r : -1; };
   auto scale_of = [&](int r) { return r >= 0 ? __ldg(p.b_scale + r) : 0.f; };
@@ -527,10 +528,12 @@ __device__ __forceinline__ void stream_consume(StreamBars& s, const StreamParams
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       tc_fence_after();
-      of(row_of(t), b[u], s.tmem_base + a * N + (uint32_t(q * 32) << 16));
+      load(s.tmem_base + a * N + (uint32_t(q * 32) << 16));
+      tmem_ld_wait();
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&s.acc_empty[a]));
+      use(row_of(t), b[u]);
       b[u] = scale_of(row_of(t + kAhead));
     }
   }
@@ -541,11 +544,11 @@ __global__ void __launch_bounds__(kStreamThreads + (OWN ? 32 * kStreamOwnWarps :
 int8_stream_kernel(const __grid_constant__ CUtensorMap tmTokens, const __grid_constant__ CUtensorMap tmRows, const StreamParams p, DevStatus* status) {
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) StreamBars bars;
-  __shared__ float a_s[4][N];   // a copy per warp; OWN: the first
+  __shared__ float a_s[8][N / 2];   // a copy of its half per warp; OWN: the first two, of all
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t tokens = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t ring = tokens + (uint32_t)p.k_blocks * N * 128u;
-  stream_begin<N>(bars, OWN ? &tmRows : &tmTokens, &tmRows, 4, OWN ? 4 + kStreamOwnWarps : 1);
+  stream_begin<N>(bars, OWN ? &tmRows : &tmTokens, &tmRows, 8, OWN ? 8 + kStreamOwnWarps : 1);
   const int r0 = (int)((long long)p.V * blockIdx.x / gridDim.x), r1 = (int)((long long)p.V * (blockIdx.x + 1) / gridDim.x);
   const int tiles = (r1 - r0 + p.rows - 1) / p.rows;
 
@@ -554,12 +557,14 @@ int8_stream_kernel(const __grid_constant__ CUtensorMap tmTokens, const __grid_co
   } else if (warp == 1) {
     if (lane == 0) stream_multiply<N>(bars, p, tokens, ring, tiles, status);
   } else {
-    float* scales = a_s[OWN ? 0 : warp & 3];
+    constexpr int kMine = N / 2;
+    const int first = (warp - 2) / 4 * kMine;   // of this warp's tokens
+    float* scales = a_s[OWN ? 0 : warp - 2];
     bool ok = true;
     if constexpr (OWN) {
       // rows of the swizzled operand: 128 bytes of a k-block, 16-byte chunk j of row t at position j ^ (t & 7).  What lies behind the
       // tokens, and behind d (where B reads as zeros), may hold anything
-      for (int t = warp - 2; t < p.T; t += 4 + kStreamOwnWarps) {
+      for (int t = warp - 2; t < p.T; t += 8 + kStreamOwnWarps) {
         const float sc = quantize_row<16>(p.X + t * p.ldX, p.d / 8, lane, [&](int v, uint2 w) {
           const uint32_t to = tokens + (uint32_t)(v >> 4) * (N * 128u) + t * 128u + ((uint32_t(v >> 1 & 7) ^ uint32_t(t & 7)) << 4) + (v & 1) * 8u;
           asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(to), "r"(w.x), "r"(w.y) : "memory");
@@ -569,32 +574,44 @@ int8_stream_kernel(const __grid_constant__ CUtensorMap tmTokens, const __grid_co
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&bars.tokens));
-      if (warp < 6) {
+      if (warp < 10) {
         ok = mbar_wait_bounded(smem_u32(&bars.tokens), 0, &bars.abort_flag);   // every lane: the scales are then visible to it
         ok = __all_sync(0xffffffffu, ok);
       }
+      scales += first;
     } else {
-      for (int t = lane; t < N; t += 32) scales[t] = t < p.T ? p.a_scale[t] : 0.f;
+      if (lane < kMine) scales[lane] = first + lane < p.T ? p.a_scale[first + lane] : 0.f;
       __syncwarp();
     }
-    if (warp < 6 && ok) {
-      stream_consume<N>(bars, p, r0, r1, tiles, status, [&](int r, float b, uint32_t taddr) {
-        const size_t out = r >= 0 ? (size_t)r : 0;
-        constexpr int kStep = N % 32 ? 16 : 32;
-#pragma unroll 1
-        for (int c = 0; c < N; c += kStep) {
-          if (c >= p.T) break;
-          uint32_t x[kStep];
-          if constexpr (kStep == 16) tmem_ld_32x16(taddr + c, x);
-          else tmem_ld_32x32(taddr + c, x);
-          tmem_ld_wait();
-          if (r >= 0) {
+    if (warp < 10 && ok && first < p.T) {
+      uint32_t x[kMine / 8][8];
+      stream_consume<N>(bars, p, r0, r1, tiles, status,
+        [&](uint32_t taddr) {
 #pragma unroll
-            for (int i = 0; i < kStep; ++i)
-              if (c + i < p.T) store_one<OUT>(p.C, out + (size_t)(c + i) * p.ldC, (float)(int)x[i] * scales[c + i] * b);
+          for (int c = 0; c < kMine / 8; ++c) tmem_ld_32x8(taddr + first + c * 8, x[c]);
+        },
+        [&](int r, float b) {
+          if (r < 0) return;
+          size_t out = (size_t)r + (size_t)first * p.ldC;
+#pragma unroll
+          for (int c = 0; c < kMine / 8; ++c) {
+            const int left = p.T - first - c * 8;   // of the tokens
+            if (left <= 0) break;
+            float z[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[i] = (float)(int)x[c][i] * scales[c * 8 + i] * b;
+            if (left >= 8) {
+#pragma unroll
+              for (int i = 0; i < 8; ++i, out += p.ldC) store_one<OUT>(p.C, out, z[i]);
+            } else {
+#pragma unroll
+              for (int i = 0; i < 8; ++i, out += p.ldC)
+                if (i < left) store_one<OUT>(p.C, out, z[i]);
+            }
           }
-        }
-      });
+        });
+    } else if (warp < 10 && ok) {
+      stream_consume<N>(bars, p, r0, r1, tiles, status, [](uint32_t) {}, [](int, float) {});   // no token is this warp's
     }
   }
   stream_end<N>(bars);
@@ -606,9 +623,8 @@ int8_stream_kernel(const __grid_constant__ CUtensorMap tmTokens, const __grid_co
 // For kStreamScores tokens: a call with this / with the engine's statistics, 151936 rows, d = 256 / 1024 / 2048: 1 token 18.5 / 39.6 / 60.7 us, 30.5 /
 // 45.0 / 68.4; 32 tokens 21.1 / 38.8 / 61.4, 28.9 / 42.3 / 65.3; but 48 tokens 26.7 / 47.3 / 67.5, 28.9 / 42.0 / 65.2, and 64 slower throughout.
 constexpr int kStreamScores = 32;
-constexpr int kStreamStatsThreads = 64 + 8 * 32;
 template <int N>
-__global__ void __launch_bounds__(kStreamStatsThreads, 1)
+__global__ void __launch_bounds__(kStreamThreads, 1)
 int8_stream_stats_kernel(const __grid_constant__ CUtensorMap tmTokens, const __grid_constant__ CUtensorMap tmRows, const StreamParams p,
                          const int* tokens_c, float4* partials, int part_stride, DevStatus* status) {
   extern __shared__ uint8_t smem_raw[];
@@ -627,7 +643,7 @@ int8_stream_stats_kernel(const __grid_constant__ CUtensorMap tmTokens, const __g
   const int r0 = (int)((long long)p.V * blockIdx.x / gridDim.x), r1 = (int)((long long)p.V * (blockIdx.x + 1) / gridDim.x);
   const int tiles = n > 0 ? (r1 - r0 + p.rows - 1) / p.rows : 0;
   if (blockIdx.x == 0 && threadIdx.x == 0) status->n_ranges = gridDim.x;
-  for (int t = threadIdx.x; t < N; t += kStreamStatsThreads) {
+  for (int t = threadIdx.x; t < N; t += kStreamThreads) {
     a_s[t] = t < n ? p.a_scale[t] : 0.f;
     y_s[t] = t < n ? tokens_c[t] : -1;
     zy_s[t] = 0.f;
@@ -643,28 +659,26 @@ int8_stream_stats_kernel(const __grid_constant__ CUtensorMap tmTokens, const __g
     float m[kMine], s[kMine], a[kMine];
 #pragma unroll
     for (int i = 0; i < kMine; ++i) { m[i] = -CUDART_INF_F; s[i] = a[i] = 0.f; }
-    stream_consume<N>(bars, p, r0, r1, tiles, status, [&](int r, float b, uint32_t taddr) {
+    uint32_t x[kMine / 8][8];
+    stream_consume<N>(bars, p, r0, r1, tiles, status,
+      [&](uint32_t taddr) {
 #pragma unroll
-      for (int c = 0; c < kMine; c += 8) {
-        uint32_t x[8];
-        tmem_ld_32x8(taddr + first + c, x);
-        tmem_ld_wait();
-        if (r >= 0) {
+        for (int c = 0; c < kMine / 8; ++c) tmem_ld_32x8(taddr + first + c * 8, x[c]);
+      },
+      [&](int r, float b) {
+        if (r < 0) return;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int t = c + i;
-            const float z = (float)(int)x[i] * a_s[first + t] * b;
-            if (r == y_s[first + t]) zy_s[first + t] = z;
-            // the smaller of the two exponents is 0
-            const float d = z - m[t], e = ex2_approx(-fabsf(d) * kLog2e);
-            const bool up = d > 0.f;
-            s[t] = up ? fmaf(s[t], e, 1.f) : s[t] + e;
-            a[t] = up ? fmaf(a[t], e, z) : fmaf(e, z, a[t]);
-            m[t] = fmaxf(m[t], z);
-          }
+        for (int t = 0; t < kMine; ++t) {
+          const float z = (float)(int)x[t / 8][t % 8] * a_s[first + t] * b;
+          if (r == y_s[first + t]) zy_s[first + t] = z;
+          // the smaller of the two exponents is 0
+          const float d = z - m[t], e = ex2_approx(-fabsf(d) * kLog2e);
+          const bool up = d > 0.f;
+          s[t] = up ? fmaf(s[t], e, 1.f) : s[t] + e;
+          a[t] = up ? fmaf(a[t], e, z) : fmaf(e, z, a[t]);
+          m[t] = fmaxf(m[t], z);
         }
-      }
-    });
+      });
     // over the warp's rows; a thread without a row has m = -inf and sums of 0
 #pragma unroll
     for (int t = 0; t < kMine; ++t) {
@@ -681,7 +695,7 @@ int8_stream_stats_kernel(const __grid_constant__ CUtensorMap tmTokens, const __g
     }
   }
   __syncthreads();
-  for (int t = threadIdx.x; t < n; t += kStreamStatsThreads) {
+  for (int t = threadIdx.x; t < n; t += kStreamThreads) {
     float4 x = part_s[t];
 #pragma unroll
     for (int w = 1; w < 4; ++w) {

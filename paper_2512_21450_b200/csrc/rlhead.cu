@@ -751,7 +751,7 @@ rl_status run_forward(rl_ctx* c, const WsLayout& L, const void* H, int64_t ldH, 
       return RL_ERR_CUDA;
     const int pr = prof_begin(c, 0);
     auto go = [&](auto kernel) {
-      launch_smem(c, kernel, blocks, kStreamStatsThreads, kStreamSmem, tmA, tmB, p, tokens_c, reinterpret_cast<float4*>(ws + L.partials), L.Tpad, c->dstatus);
+      launch_smem(c, kernel, blocks, kStreamThreads, kStreamSmem, tmA, tmB, p, tokens_c, reinterpret_cast<float4*>(ws + L.partials), L.Tpad, c->dstatus);
     };
     if (n == 16) go(int8_stream_stats_kernel<16>);
     else go(int8_stream_stats_kernel<32>);
