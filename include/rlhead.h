@@ -494,8 +494,8 @@ rl_status rl_quantize_rows(rl_ctx* ctx, const void* X, int x_dtype, int64_t ldX,
  * (rl_quantize_rows) into the workspace (rl_workspace_bytes_int8_linear) first: the logits of hidden states under a head held in 8
  * bits.  A, B: 16-byte aligned, row strides multiples of 16 (the 16-byte words that a row's last elements lie in are read whole);
  * d < 2^17, any number.  b_scale 16-byte aligned.  C: row stride ldC >= V elements, what lies between V and ldC is left alone;
- * rows that start and end on 16 bytes are written faster.  Up to 64 tokens are a stream of B past tokens that stay in shared memory, more run in
- * tiles of 256 rows.  T = 0 is not an error.
+ * rows that start and end on 16 bytes are written faster.  Up to 128 tokens are a stream of B past tokens that stay in shared memory as
+ * long as they fit, more run in tiles of 256 rows.  T = 0 is not an error.
  * Errors: unknown type, NULL pointers -> RL_ERR_INVALID_ARG; RL_ERR_SHAPE; RL_ERR_ALIGNMENT; RL_ERR_WORKSPACE (rl_int8_linear). */
 rl_status rl_int8_matmul(rl_ctx* ctx, const int8_t* A, int64_t ldA, const float* a_scale, const int8_t* B, int64_t ldB,
                          const float* b_scale, int64_t T, int64_t d, int64_t V, void* C, int c_dtype, int64_t ldC);

@@ -359,21 +359,25 @@ struct EpiScale {
 };
 
 // ---------------------------------------------------------------------------------------------
-// Up to N tokens as a stream of B on the tensor cores, the operands' roles exchanged: 128 rows of B are the M side of a tile, the tokens
+// Up to N tokens (at most 128) as a stream of B on the tensor cores, the operands' roles exchanged: 128 rows of B are the M side of a tile, the tokens
 // its N side.  All of the tokens lie in shared memory for the whole kernel.  (As the M side of the engine's tiles they were read again
 // for every tile by every CTA, which made the L2 slices of a few lines the bottleneck: 9 to 32 tokens took 110 to 140 us at
 // d = 3584 and 152 K rows, 40 to 128 took 97 to 101; a dp4a kernel took 95 us for one token and 139 for eight.)  Every CTA takes an equal share of the rows in tiles of `rows`.
 //   warp 0: TMA producer;  warp 1: allocates tensor memory, issues the products;  warps 2 to 9: a thread per row of B and half of the tokens.
 constexpr int kStreamStageBytes = 128 * 128;   // 128 rows, a k-block of 128 bytes
-constexpr int kStreamMaxStages = 12, kStreamMinStages = 4;
+constexpr int kStreamMaxStages = 12;
 constexpr int kStreamSmem = 224 * 1024;        // of it 1 KB to start on a multiple of 1024
 constexpr int kStreamThreads = 64 + 8 * 32;
-// Stages that fit beside the tokens; fewer than kStreamMinStages: too many tokens for this kernel.
+// Stages that fit beside the tokens.
 __host__ __device__ constexpr int stream_stages(int n_tokens, int k_blocks) {
   const long long left = kStreamSmem - 1024 - (long long)n_tokens * 128 * k_blocks;
   const long long s = left < 0 ? 0 : left / kStreamStageBytes;
   return (int)(s < kStreamMaxStages ? s : kStreamMaxStages);
 }
+// Fewer stages than these and the engine's tiles are faster.  151936 rows, 65 / 96 tokens, stream / engine: d = 448 17.1 / 17.9 us, 20.9 / 22.9; d = 1024
+// 32.3 / 34.0, 37.2 / 37.5; d = 1280 (six stages) 39.2 / 41.3, 46.7 / 43.8; d = 1664 (four) 54.0 / 55.8, 60.6 / 53.8.  128 tokens: d = 448 21.2, 23.6;
+// d = 1024 36.9, 38.9; d = 1152 (four) 43.0, 43.2.  64 tokens at d = 2560 (three) 83, 73-88; 48 at d = 2560 (six) 69, 88.
+constexpr int stream_min_stages(int n_tokens) { return n_tokens > 64 ? 5 : 4; }
 // Up to kStreamOwn tokens in bf16 the kernel quantises itself, in four warps more and before these eight turn to their rows, while the ring
 // fills: a launch less.  1 / 4 / 8 / 13 / 16 tokens, 151936 rows, d = 2048 52.8 / 54.3 / 55.5 / 55.8 / 56.0 us with the launch, 50.0 / 51.7 / 52.7 / 53.1 /
 // 53.6 without; d = 3584 88.0 / 90.5 / 92.4 / 93.4 / 93.5, 83.3 / 85.3 / 86.4 / 88.6 / 89.4.
@@ -395,7 +399,7 @@ struct StreamBars {
   int abort_flag;
 };
 template <int N>
-constexpr uint32_t kStreamCols = 2 * N <= 32 ? 32 : 2 * N <= 64 ? 64 : 128;   // two accumulators; a power of two from 32 on
+constexpr uint32_t kStreamCols = 2 * N <= 32 ? 32 : 2 * N <= 64 ? 64 : 2 * N <= 128 ? 128 : 256;   // two accumulators; a power of two from 32 on
 // Before the launch's memory is touched.  acc_warps: warps that read an accumulator; token_arrivals: on the barrier of the tokens.
 template <int N>
 __device__ __forceinline__ void stream_begin(StreamBars& s, const CUtensorMap* tmTokens, const CUtensorMap* tmRows, int acc_warps, int token_arrivals) {
@@ -580,7 +584,7 @@ int8_stream_kernel(const __grid_constant__ CUtensorMap tmTokens, const __grid_co
       }
       scales += first;
     } else {
-      if (lane < kMine) scales[lane] = first + lane < p.T ? p.a_scale[first + lane] : 0.f;
+      for (int t = lane; t < kMine; t += 32) scales[t] = first + t < p.T ? p.a_scale[first + t] : 0.f;
       __syncwarp();
     }
     if (warp < 10 && ok && first < p.T) {

@@ -436,6 +436,8 @@ cudaError_t set_smem_attr_int8() {
   stream_out(std::integral_constant<int, 32>());
   stream_out(std::integral_constant<int, 48>());
   stream_out(std::integral_constant<int, 64>());
+  stream_out(std::integral_constant<int, 96>());
+  stream_out(std::integral_constant<int, 128>());
   return e;
 }
 
@@ -647,8 +649,11 @@ void launch_mask_scan(rl_ctx* c, const uint8_t* mask, int64_t T, int* block_coun
 }
 
 // Few tokens: the N side of the stream's tiles, and whether they fit beside a ring.
-inline int stream_tokens(int64_t T) { return T <= 16 ? 16 : T <= 32 ? 32 : T <= 48 ? 48 : 64; }
-inline bool streams(int64_t T, int64_t d) { return T <= 64 && stream_stages(stream_tokens(T), (int)((d + 127) / 128)) >= kStreamMinStages; }
+inline int stream_tokens(int64_t T) { return T <= 16 ? 16 : T <= 32 ? 32 : T <= 48 ? 48 : T <= 64 ? 64 : T <= 96 ? 96 : 128; }
+inline bool streams(int64_t T, int64_t d) {
+  const int n = stream_tokens(T);
+  return T <= 128 && stream_stages(n, (int)((d + 127) / 128)) >= stream_min_stages(n);
+}
 
 // Shape of a stream of B on at most `most` blocks; the blocks.
 inline int stream_shape(StreamParams& p, const float* b_scale, int64_t T, int64_t d, int64_t V, int most) {
@@ -1951,7 +1956,9 @@ static rl_status int8_stream(rl_ctx* c, const CUtensorMap* tokens, StreamParams 
   else if (n == 16) of(std::integral_constant<int, 16>());
   else if (n == 32) of(std::integral_constant<int, 32>());
   else if (n == 48) of(std::integral_constant<int, 48>());
-  else of(std::integral_constant<int, 64>());
+  else if (n == 64) of(std::integral_constant<int, 64>());
+  else if (n == 96) of(std::integral_constant<int, 96>());
+  else of(std::integral_constant<int, 128>());
   prof_end(c, pr, 0);
   c->launches++;
   return cuda_ok();

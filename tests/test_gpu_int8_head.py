@@ -100,7 +100,8 @@ def _int8(T, d, seed, lo=-128):
 
 PRODUCTS = [(1, 1, 1), (1, 64, 7), (2, 17, 33), (3, 2048, 1000), (4, 100, 515), (5, 33, 2), (8, 1000, 4099), (7, 8000, 300), (8, 8192, 77),
             (8, 8193, 65), (9, 64, 1), (9, 1, 300), (16, 129, 256), (128, 256, 1000), (129, 256, 1000), (200, 1000, 4099), (300, 2048, 513), (257, 127, 8),
-            (12, 3584, 40000), (33, 100, 1000), (40, 2048, 515), (64, 1024, 20011), (65, 130, 149), (100, 1024, 1500), (128, 900, 148), (17, 12000, 700), (33, 2560, 900), (48, 3200, 151), (64, 2432, 333)]
+            (12, 3584, 40000), (33, 100, 1000), (40, 2048, 515), (64, 1024, 20011), (65, 130, 149), (100, 1024, 1500), (128, 900, 148), (17, 12000, 700), (33, 2560, 900), (48, 3200, 151), (64, 2432, 333), (96, 1408, 700), (81, 1500, 515),
+            (128, 1024, 4099), (128, 1025, 300), (97, 256, 40000)]
 
 
 @pytest.mark.parametrize("T,d,V", PRODUCTS)
