@@ -347,6 +347,27 @@ def test_scoring_nothing_that_counts(ctx, T):
     _ok(ctx)
 
 
+@pytest.mark.parametrize("T", [5, 30, 77, 300])
+def test_scoring_of_rows_that_are_not_finite(ctx, T):
+    """Such a row's results are NaN, every other row's what they are without it."""
+    W = _rows(2000, 256, torch.bfloat16, seed=1, std=0.05)
+    H = _rows(T, 256, torch.bfloat16, seed=2)
+    tok = torch.randint(0, 2000, (T,), device=DEV, dtype=torch.int32)
+    Wq, ws = ctx.rl_quantize_rows(W)
+    want = ctx.rl_token_logprobs_int8(H, Wq, ws, tok)
+    bad = H.clone()
+    bad[1, 9], bad[3, 0] = float("nan"), float("-inf")
+    keep = torch.ones(T, dtype=torch.bool, device=DEV)
+    keep[1] = keep[3] = False
+    for x, w in zip(ctx.rl_token_logprobs_int8(bad, Wq, ws, tok), want):
+        assert bool(torch.isnan(x[~keep]).all()) and torch.equal(x[keep], w[keep])
+    zero = H.clone()
+    zero[2] = 0                                       # logits of zero: the uniform distribution
+    logp, ent, lse = ctx.rl_token_logprobs_int8(zero, Wq, ws, tok)
+    log_v = torch.log(torch.tensor(2000.0)).item()
+    assert max(abs(logp[2].item() + log_v), abs(ent[2].item() - log_v), abs(lse[2].item() - log_v)) <= 1e-5
+
+
 def test_weights_written_just_before(ctx):
     """The weights are fetched ahead of the tokens, but not ahead of the launch that writes them."""
     base = [ctx.rl_quantize_rows(_rows(40000, 1024, torch.bfloat16, seed=s, std=0.05)) for s in (1, 2)]
