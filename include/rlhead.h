@@ -492,8 +492,8 @@ rl_status rl_quantize_rows(rl_ctx* ctx, const void* X, int x_dtype, int64_t ldX,
 /* Product of 8-bit rows: C[t,v] = a_scale[t] b_scale[v] sum_k A[t,k] B[v,k], in bf16, fp32 or fp16.  The sums are exact; they are
  * rounded to fp32, multiplied by a_scale[t], then by b_scale[v], then rounded to C's type.  rl_int8_linear quantises the rows of X
  * (rl_quantize_rows) into the workspace (rl_workspace_bytes_int8_linear) first: the logits of hidden states under a head held in 8
- * bits.  A, B: 16-byte aligned, row strides multiples of 16 (the 16-byte words that a row's last elements lie in are read whole);
- * d < 2^17, any number.  b_scale 16-byte aligned.  C: row stride ldC >= V elements, what lies between V and ldC is left alone;
+ * bits.  A, B: 16-byte aligned, row strides multiples of 16, what lies between d and them is not read;
+ * d < 2^17, any number.  C: row stride ldC >= V elements, what lies between V and ldC is left alone;
  * rows that start and end on 16 bytes are written faster.  Up to 128 tokens are a stream of B past tokens that stay in shared memory as
  * long as they fit, more run in tiles of 256 rows.  T = 0 is not an error.
  * Errors: unknown type, NULL pointers -> RL_ERR_INVALID_ARG; RL_ERR_SHAPE; RL_ERR_ALIGNMENT; RL_ERR_WORKSPACE (rl_int8_linear). */
@@ -503,7 +503,7 @@ rl_status rl_workspace_bytes_int8_linear(rl_ctx* ctx, int64_t T, int64_t d, size
 rl_status rl_int8_linear(rl_ctx* ctx, const void* X, int x_dtype, int64_t ldX, const int8_t* B, int64_t ldB, const float* b_scale,
                          int64_t T, int64_t d, int64_t V, void* C, int c_dtype, int64_t ldC);
 
-/* rl_token_logprobs under a head held in 8 bits: W [V,d] int8_t with w_scale[V] (16-byte aligned), ldW a multiple of 16; the valid rows
+/* rl_token_logprobs under a head held in 8 bits: W [V,d] int8_t with w_scale[V], ldW a multiple of 16; the valid rows
  * of H (bf16) are quantised as they are compacted.  Logits are those of rl_int8_linear before their last rounding and are not
  * kept.  Twice the tensor throughput and half the bytes of W.  Workspace: rl_workspace_bytes_logprobs. */
 rl_status rl_token_logprobs_int8(rl_ctx* ctx, const void* H, int64_t ldH, const int8_t* W, int64_t ldW, const float* w_scale,

@@ -1929,7 +1929,7 @@ static rl_status check_int8(const void* B, int64_t ldB, const float* b_scale, in
   // 2^17 - 1 products of -128 with -128 still fit 32 bits
   if (d >= (1 << 17) || T >= (int64_t(1) << 30) || V >= (int64_t(1) << 30) || ldB < d || ldC < V) return RL_ERR_SHAPE;
   const uintptr_t elem = c_dtype == RL_FP32 ? 4 : 2;
-  if ((reinterpret_cast<uintptr_t>(B) & 15) || ldB % 16 || (reinterpret_cast<uintptr_t>(b_scale) & 15) || reinterpret_cast<uintptr_t>(C) % elem)
+  if ((reinterpret_cast<uintptr_t>(B) & 15) || ldB % 16 || (reinterpret_cast<uintptr_t>(b_scale) & 3) || reinterpret_cast<uintptr_t>(C) % elem)
     return RL_ERR_ALIGNMENT;
   return RL_OK;
 }
@@ -2038,7 +2038,7 @@ rl_status rl_token_logprobs_int8(rl_ctx* c, const void* H, int64_t ldH, const in
   rl_status s = check_hw(H, ldH, W, ldW, T, d, V);
   if (s != RL_OK) return s;
   if (d >= (1 << 17)) return RL_ERR_SHAPE;
-  if (ldW % 16 || (reinterpret_cast<uintptr_t>(w_scale) & 15)) return RL_ERR_ALIGNMENT;
+  if (ldW % 16 || (reinterpret_cast<uintptr_t>(w_scale) & 3)) return RL_ERR_ALIGNMENT;
   if (T == 0) return RL_OK;
   if (!tokens || !logp || !w_scale) return RL_ERR_INVALID_ARG;
   const OnDevice on(c);

@@ -474,5 +474,18 @@ def test_what_the_native_half_leaves_to_the_general_path(ctx):
         ctx.rl_cross_entropy_fwd_bwd(X, W, torch.zeros(10, dtype=torch.int32, device=DEV), label_smoothing=1.0)
     assert e.value.status == 1
     with pytest.raises(RLHeadError) as e:
-        ctx.rl_int8_linear(X, Q, torch.ones(61, device=DEV)[1:])      # scales that start on 4 bytes
+        ctx.rl_int8_linear(X, torch.zeros(60, 144, dtype=torch.int8, device=DEV)[:, 8:136], s)      # rows that start on 8 bytes
     assert e.value.status == 3
+
+
+@pytest.mark.parametrize("T", [3, 40, 70, 300])
+def test_slices_of_a_head(ctx, T):
+    """Rows of a head from any one on, as a rank of a head that is split by vocabulary holds them: their scales start anywhere."""
+    X, W = _rows(T, 256, torch.bfloat16, seed=1), _rows(900, 256, torch.bfloat16, seed=2, std=0.1)
+    Q, s = ctx.rl_quantize_rows(W)
+    whole = ctx.rl_int8_linear(X, Q, s, out_dtype=torch.float32)
+    tok = torch.randint(0, 300, (T,), device=DEV, dtype=torch.int32)
+    for a, b in ((0, 900), (1, 302), (301, 900), (599, 900)):
+        assert torch.equal(ctx.rl_int8_linear(X, Q[a:b], s[a:b], out_dtype=torch.float32), whole[:, a:b])
+        lse = ctx.rl_token_logprobs_int8(X, Q[a:b], s[a:b], tok)[2]
+        assert (lse - torch.logsumexp(whole[:, a:b].double(), 1)).abs().max().item() <= 1e-6 * (lse.abs().max().item() + 12)

@@ -76,7 +76,7 @@ def test_product_refusals(lib, ctx):
             assert call(**kw) == INVALID, kw
         for kw in (dict(ldB=96), dict(ldC=49), dict(T=1 << 30), dict(V=1 << 30, ldC=1 << 30), dict(d=1 << 17, ldB=1 << 17)):
             assert call(**kw) == SHAPE, kw
-        for kw in (dict(B=A + 8), dict(ldB=120), dict(b=A + 4), dict(C=A + 1), dict(t=1, C=A + 2)):
+        for kw in (dict(B=A + 8), dict(ldB=120), dict(b=A + 2), dict(C=A + 1), dict(t=1, C=A + 2)):
             assert call(**kw) == ALIGN, kw
         assert call(T=0, C=None) == OK
     for kw in (dict(X=None), dict(a=None)):
@@ -101,7 +101,7 @@ def test_scoring_refusals(lib, ctx):
         assert call(**kw) == INVALID, kw
     for kw in (dict(d=100), dict(ldH=64), dict(ldW=112), dict(d=1 << 17, ldH=1 << 17, ldW=1 << 17)):
         assert call(**kw) == SHAPE, kw
-    for kw in (dict(ldW=136), dict(W=A + 8), dict(H=A + 8), dict(s=A + 4)):
+    for kw in (dict(ldW=136), dict(W=A + 8), dict(H=A + 8), dict(s=A + 2)):
         assert call(**kw) == ALIGN, kw
     assert call(T=0) == OK
 
