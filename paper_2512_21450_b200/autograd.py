@@ -62,7 +62,8 @@ class _FusedCrossEntropy(torch.autograd.Function):
 def fused_cross_entropy(H, W, targets, mask=None, label_smoothing=0.0, z_coef=0.0, token_weight=None, token_count=None):
     """Supervised loss of `targets` as a differentiable scalar in H [T,d] bf16 and W [V,d] bf16: (loss, logp[T]).
 
-    Gradients (bf16) are formed with the loss, for those of H and W that ask for one.
+    Gradients (bf16) are formed with the loss, for those of H and W that ask for one.  A step that is to be captured into a CUDA graph
+    calls rl_cross_entropy_fwd_bwd, which hands loss and gradients over without autograd's own streams and events.
     """
     grad = torch.is_grad_enabled()
     return _FusedCrossEntropy.apply(H, W, targets, mask, label_smoothing, z_coef, token_weight, token_count,
