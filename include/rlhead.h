@@ -60,6 +60,11 @@ typedef struct rl_ctx rl_ctx;  /* opaque; one per device and stream */
 rl_status rl_create(rl_ctx** out, int device);
 rl_status rl_destroy(rl_ctx* ctx);
 rl_status rl_set_stream(rl_ctx* ctx, void* cuda_stream);
+/* The same for a context whose present stream still exists, in order: what the present stream has been given comes before what the
+ * new one is given from now on, so that calls which share the context's workspace and device block take turns (rl_set_stream
+ * leaves that to the caller).  Where both streams are being captured into one graph the graph gets that order; a stream that is
+ * being captured and one that is not have none, since a graph runs when it is replayed: order replays with the context's other calls. */
+rl_status rl_follow_stream(rl_ctx* ctx, void* cuda_stream);
 const char* rl_status_string(rl_status s);
 
 /* Bytes of scratch needed by any call with at most T rows, hidden size d, vocabulary V.  The

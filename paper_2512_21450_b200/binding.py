@@ -94,6 +94,7 @@ def load_library():
     lib.rl_status_string.argtypes = [c_int]
     lib.rl_create.argtypes = [POINTER(c_void_p), c_int]
     lib.rl_destroy.argtypes = [P]
+    lib.rl_follow_stream.argtypes = [P, P]
     lib.rl_set_stream.argtypes = [P, P]
     lib.rl_workspace_bytes.argtypes = [P, c_int64, c_int64, c_int64, POINTER(c_size_t)]
     lib.rl_workspace_bytes_host.argtypes = [P, c_int64, c_int64, c_int64, POINTER(c_size_t)]
@@ -179,7 +180,7 @@ def load_library():
     lib.rl_workspace_bytes_int8_linear.argtypes = [P, c_int64, c_int64, POINTER(c_size_t)]
     lib.rl_int8_linear.argtypes = [P, P, c_int, c_int64, P, c_int64, P, c_int64, c_int64, c_int64, P, c_int, c_int64]
     lib.rl_token_logprobs_int8.argtypes = [P, P, c_int64, P, c_int64, P, P, P, c_int64, c_int64, c_int64, P, P, P]
-    for name in ("rl_create", "rl_destroy", "rl_set_stream", "rl_workspace_bytes", "rl_workspace_bytes_host",
+    for name in ("rl_create", "rl_destroy", "rl_set_stream", "rl_follow_stream", "rl_workspace_bytes", "rl_workspace_bytes_host",
                  "rl_workspace_bytes_kl", "rl_workspace_bytes_logprobs",
                  "rl_set_workspace", "rl_set_slab_limits", "rl_last_device_status", "rl_grpo_advantages", "rl_grpo_advantages_ex",
                  "rl_token_logprobs", "rl_policy_loss_fwd_bwd", "rl_policy_loss_fwd_bwd_ex",
@@ -275,9 +276,14 @@ def _check(status, where):
 
 class Context:
     """One library context on one device; owns a torch-allocated workspace.  A workspace that calls were captured with into a CUDA graph
-    stays allocated as long as the context does, also when a larger one takes its place: the graph writes to it at every replay."""
+    stays allocated as long as the context does, also when a larger one takes its place: the graph writes to it at every replay.
+
+    Calls run on torch's current stream.  Where that is another one than at the call before, they still follow one another, since they share
+    the workspace: streams that are to work side by side have a context each.  Replays of graphs are calls that the context does not
+    see: whoever replays orders them with each other and with the context's other calls.  One thread at a time."""
 
     _captured, _kept = False, ()   # whether calls were captured with the present workspace; earlier ones that calls were captured with
+    _foreign = False               # whether the stream that calls ran on last belongs to somebody else than torch
 
     def __init__(self, device=0):
         if not torch.cuda.is_available():
@@ -311,8 +317,21 @@ class Context:
         if torch._C._cuda_isCurrentStreamCapturing():
             self._captured = True
         if stream != self._stream:
+            self._change_stream(stream)
+
+    def _change_stream(self, stream):
+        now = torch.cuda.current_stream(self.device)
+        capturing = torch._C._cuda_isCurrentStreamCapturing()
+        if self._stream is None or (self._foreign and capturing):
             _check(self.lib.rl_set_stream(self.handle, stream), "rl_set_stream")
-            self._stream = stream
+        elif self._foreign:
+            # its owner may have destroyed it: no event can be recorded on it any more
+            torch.cuda.synchronize(self.device)
+            _check(self.lib.rl_set_stream(self.handle, stream), "rl_set_stream")
+        else:
+            _check(self.lib.rl_follow_stream(self.handle, stream), "rl_follow_stream")
+        self._stream = stream
+        self._foreign = stream != 0 and now.stream_id == stream   # the id of a stream that is not torch's is its handle
 
     def _need_workspace(self, nbytes):
         if self._ws is None or self._ws.numel() < nbytes:

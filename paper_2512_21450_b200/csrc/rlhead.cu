@@ -55,6 +55,7 @@ struct rl_ctx {
   cudaEvent_t copy_done[2], step_done[2];
   float* pinned_out[2];
   int slot_busy[2];
+  cudaEvent_t turn;               // what a stream has been given that the context leaves (rl_follow_stream)
   int* prof_kind;                 // [kProfMax], allocated when profiling is first switched on
   cudaEvent_t (*prof_ev)[2];      // [kProfMax][2], events created on first use
 };
@@ -897,6 +898,7 @@ rl_status rl_create(rl_ctx** out, int device) {
             set_smem_attr<EpiAccScatter<8, kAccHalf>, 1, 1>() == cudaSuccess && set_smem_attr<EpiAccW<4, kAccScaled>, 1, 1>() == cudaSuccess &&
             set_smem_attr<EpiAccScatter<4, kAccScaled>, 1, 1>() == cudaSuccess && set_smem_attr<EpiAccScatter<8, kAccScaled>, 1, 1>() == cudaSuccess && set_smem_attr<EpiAccSlabs, 1, 1>() == cudaSuccess &&
             set_smem_attr<EpiScatterWith<EpiAccSlabs>, 1, 1>() == cudaSuccess && set_smem_attr_int8() == cudaSuccess;
+  ok = ok && cudaEventCreateWithFlags(&c->turn, cudaEventDisableTiming) == cudaSuccess;
   if (!ok) { cudaFree(c->dstatus); delete c; return RL_ERR_CUDA; }
   {
     // how many CTA pairs can be resident at once (pairs must share a TPC): the persistent grid
@@ -948,6 +950,7 @@ rl_status rl_destroy(rl_ctx* c) {
       cudaFreeHost(c->pinned_out[i]);
     }
   }
+  cudaEventDestroy(c->turn);
   cudaFree(c->dstatus);
   delete c;
   return RL_OK;
@@ -956,6 +959,28 @@ rl_status rl_destroy(rl_ctx* c) {
 rl_status rl_set_stream(rl_ctx* c, void* s) {
   if (!c) return RL_ERR_INVALID_ARG;
   c->stream = static_cast<cudaStream_t>(s);
+  return RL_OK;
+}
+
+rl_status rl_follow_stream(rl_ctx* c, void* s) {
+  if (!c) return RL_ERR_INVALID_ARG;
+  const cudaStream_t next = static_cast<cudaStream_t>(s);
+  if (next == c->stream) return RL_OK;
+  const OnDevice on(c);
+  // the capture that a stream is in, 0 for none; false where it cannot be asked (the legacy default stream while a stream that blocks
+  // it is captured: an event on it would end that capture)
+  auto capture = [](cudaStream_t st, unsigned long long& id) {
+    cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+    const bool known = cudaStreamGetCaptureInfo(st, &status, &id) == cudaSuccess;
+    if (!known) cudaGetLastError();
+    if (status != cudaStreamCaptureStatusActive) id = 0;
+    return known;
+  };
+  unsigned long long before = 0, after = 0;
+  if (capture(c->stream, before) && capture(next, after) && before == after &&
+      (cudaEventRecord(c->turn, c->stream) != cudaSuccess || cudaStreamWaitEvent(next, c->turn, 0) != cudaSuccess))
+    return RL_ERR_CUDA;
+  c->stream = next;
   return RL_OK;
 }
 

@@ -1,0 +1,182 @@
+"""Calls of one context from several streams: its workspace and device block are one, so they follow one another."""
+import pytest
+import torch
+
+DEV = "cuda:0"
+
+
+class _Torch:
+    """What Context asks torch for, without a device: the current stream's handle, its id and whether it is captured."""
+
+    def __init__(self, monkeypatch):
+        self.handle, self.id, self.capturing, self.synchronised = 0, 0, False, 0
+        monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: self.handle, raising=False)
+        monkeypatch.setattr(torch._C, "_cuda_isCurrentStreamCapturing", lambda: self.capturing, raising=False)
+        monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: type("Stream", (), dict(stream_id=self.id, cuda_stream=self.handle)))
+        monkeypatch.setattr(torch.cuda, "synchronize", lambda device=None: setattr(self, "synchronised", self.synchronised + 1))
+
+    def on(self, handle, id, capturing=False):
+        self.handle, self.id, self.capturing = handle, id, capturing
+
+
+class _Library:
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.calls.append((name,) + args[1:])
+            return 0
+        return call
+
+
+def _context():
+    from paper_2512_21450_b200 import Context
+    c = Context.__new__(Context)
+    c.lib, c.handle, c._address, c._ws, c._stream, c.device = _Library(), None, 0, None, None, torch.device("cuda", 0)
+    return c
+
+
+def test_a_context_that_changes_streams_follows_the_one_it_leaves(monkeypatch):
+    t, c = _Torch(monkeypatch), _context()
+    c._bind_stream()                              # the first: nothing to follow
+    t.on(0x5000, 35)                              # one of torch's streams
+    c._bind_stream()
+    c._bind_stream()                              # the same again
+    t.on(0, 0)
+    c._bind_stream()
+    t.on(0x6000, 67, capturing=True)              # the library knows what is captured
+    c._bind_stream()
+    t.on(0, 0)
+    c._bind_stream()
+    assert c.lib.calls == [("rl_set_stream", 0), ("rl_follow_stream", 0x5000), ("rl_follow_stream", 0), ("rl_follow_stream", 0x6000),
+                           ("rl_follow_stream", 0)] and t.synchronised == 0
+
+
+def test_a_stream_of_somebody_else_may_be_gone_when_it_is_left(monkeypatch):
+    t, c = _Torch(monkeypatch), _context()
+    c._bind_stream()
+    t.on(0x7000, 0x7000)                          # a stream that torch was handed: its id is its handle
+    c._bind_stream()
+    assert t.synchronised == 0
+    t.on(0x5000, 35)
+    c._bind_stream()
+    assert t.synchronised == 1 and c.lib.calls[-1] == ("rl_set_stream", 0x5000)
+    t.on(0, 0)
+    c._bind_stream()
+    assert t.synchronised == 1 and c.lib.calls[-1] == ("rl_follow_stream", 0)
+    t.on(0x7000, 0x7000)
+    c._bind_stream()
+    t.on(0x6000, 67, capturing=True)              # no synchronisation while a graph is captured
+    c._bind_stream()
+    assert t.synchronised == 1 and c.lib.calls[-1] == ("rl_set_stream", 0x6000)
+
+
+def test_no_context_is_refused():
+    from paper_2512_21450_b200 import build
+    from paper_2512_21450_b200.binding import load_library
+    build.build()
+    assert load_library().rl_follow_stream(None, None) == 1
+
+
+def _data(T, d, V, seed):
+    g = torch.Generator(DEV).manual_seed(seed)
+    H = torch.randn(T, d, generator=g, device=DEV).bfloat16()
+    W = (torch.randn(V, d, generator=g, device=DEV) * 0.05).bfloat16()
+    y = torch.randint(0, V, (T,), generator=g, device=DEV, dtype=torch.int32)
+    return H, W, y, (torch.rand(T, generator=g, device=DEV) < 0.8).to(torch.uint8)
+
+
+@pytest.mark.gpu
+def test_two_streams_through_the_module_level_functions():
+    """Different sizes on two streams, nothing synchronised in between: every result is that of a call alone."""
+    import paper_2512_21450_b200 as rl
+    H1, W1, y1, m1 = _data(900, 1024, 20000, 1)
+    H2, W2, y2, m2 = _data(300, 512, 9000, 2)
+    Wq, ws = rl.rl_quantize_rows(W2)
+
+    def loss():
+        out = rl.rl_cross_entropy_fwd_bwd(H1, W1, y1, m1, label_smoothing=0.1, z_coef=1e-4, dW_bf16=True)
+        return [out[k] for k in ("loss", "logp", "lse", "dH", "dW")]
+
+    def score():
+        return list(rl.rl_token_logprobs_int8(H2, Wq, ws, y2, m2)) + [rl.rl_int8_linear(H2[:n], Wq, ws) for n in (300, 40)]
+    want = []
+    for call in (loss, score):
+        want.append(call())
+        torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(6):
+        got.append((0, loss()))
+        with torch.cuda.stream(side):
+            got.append((1, score()))
+    torch.cuda.synchronize()
+    for i, outs in got:
+        for a, b in zip(outs, want[i]):
+            assert torch.equal(a, b), i
+    assert rl.default_context(0).last_device_status()[0] == 0
+
+
+@pytest.mark.gpu
+def test_two_streams_of_one_capture():
+    """A captured stream that forks: the graph has the calls of both branches in the order in which they were made."""
+    from paper_2512_21450_b200 import Context
+    c = Context(0)
+    try:
+        H, W, y, m = _data(400, 512, 6000, 3)
+        Wq, ws = c.rl_quantize_rows(W)
+        loss, dH, dW = torch.empty(1, device=DEV), torch.empty_like(H), torch.empty_like(W)
+        C = torch.empty(400, 6000, dtype=torch.bfloat16, device=DEV)
+        ce = lambda: c.rl_cross_entropy_fwd_bwd(H, W, y, m, loss=loss, dH=dH, dW=dW, dW_bf16=True)  # noqa: E731
+        logits = lambda: c.rl_int8_linear(H, Wq, ws, out=C)  # noqa: E731
+        ce(), logits()
+        want = [x.clone() for x in (loss, dH, dW, C)]
+        torch.cuda.synchronize()
+        side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            main = torch.cuda.current_stream()
+            side.wait_stream(main)
+            ce()
+            with torch.cuda.stream(side):
+                logits()
+            ce()
+            main.wait_stream(side)
+        for _ in range(3):
+            for x in (loss, dH, dW, C):
+                x.fill_(7)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip((loss, dH, dW, C), want))
+        assert c.last_device_status()[0] == 0
+        # calls that run follow on, and so does a stream that torch did not make
+        ce()
+        assert torch.equal(dW, want[2])
+    finally:
+        c.close()
+
+
+@pytest.mark.gpu
+def test_streams_made_by_somebody_else():
+    """Handles from the runtime, destroyed by their owner before the context is used on another stream."""
+    import ctypes
+    from paper_2512_21450_b200 import Context
+    runtime = ctypes.CDLL("libcudart.so.12")
+    c = Context(0)
+    try:
+        H, W, y, m = _data(400, 512, 6000, 4)
+        want = c.rl_cross_entropy_fwd_bwd(H, W, y, m)
+        torch.cuda.synchronize()
+        for _ in range(2):
+            handle = ctypes.c_void_p()
+            assert runtime.cudaStreamCreateWithFlags(ctypes.byref(handle), 1) == 0
+            with torch.cuda.stream(torch.cuda.ExternalStream(handle.value)):
+                a = c.rl_cross_entropy_fwd_bwd(H, W, y, m)
+            torch.cuda.synchronize()
+            assert c._foreign and runtime.cudaStreamDestroy(handle) == 0
+            b = c.rl_cross_entropy_fwd_bwd(H, W, y, m)
+            assert not c._foreign
+            assert all(torch.equal(a[k], want[k]) and torch.equal(b[k], want[k]) for k in want)
+    finally:
+        c.close()
