@@ -332,11 +332,15 @@ class Context:
             _check(self.lib.rl_follow_stream(self.handle, stream), "rl_follow_stream")
         self._stream = stream
         self._foreign = stream != 0 and now.stream_id == stream   # the id of a stream that is not torch's is its handle
+        if self._ws is not None and not capturing and not self._foreign:
+            self._ws.record_stream(now)   # when it is replaced, its memory is not handed out before this stream is through with it
 
     def _need_workspace(self, nbytes):
         if self._ws is None or self._ws.numel() < nbytes:
             if self._captured and self._ws is not None:
                 self._kept += (self._ws,)
+            elif self._foreign and self._ws is not None:
+                torch.cuda.synchronize(self.device)   # what is recorded on such a stream may outlive it
             self._captured = bool(torch._C._cuda_isCurrentStreamCapturing())
             self._ws = None
             self._ws = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=self.device)

@@ -72,6 +72,49 @@ def test_a_stream_of_somebody_else_may_be_gone_when_it_is_left(monkeypatch):
     assert t.synchronised == 1 and c.lib.calls[-1] == ("rl_set_stream", 0x6000)
 
 
+class _Workspace:
+    def __init__(self, n):
+        self.n, self.recorded = n, []
+
+    def numel(self):
+        return self.n
+
+    def data_ptr(self):
+        return 1 << 20
+
+    def record_stream(self, stream):
+        self.recorded.append(stream.cuda_stream)
+
+
+def test_every_stream_that_used_a_workspace_is_waited_for_before_its_memory_goes(monkeypatch):
+    t, c = _Torch(monkeypatch), _context()
+    monkeypatch.setattr(torch, "empty", lambda n, **kw: _Workspace(n))
+    c._bind_stream()
+    c._need_workspace(100)
+    first = c._ws
+    for handle, id in ((0x5000, 35), (0, 0), (0x6000, 67)):
+        t.on(handle, id)
+        c._bind_stream()
+        c._need_workspace(100)
+    assert c._ws is first and first.recorded == [0x5000, 0, 0x6000]
+    c._need_workspace(200)
+    assert c._ws is not first and t.synchronised == 0
+    # one that torch does not own cannot be waited for later
+    second = c._ws
+    t.on(0x7000, 0x7000)
+    c._bind_stream()
+    c._need_workspace(200)
+    assert t.synchronised == 0 and second.recorded == []
+    c._need_workspace(300)
+    assert t.synchronised == 1 and c._kept == ()
+    # one that a graph writes to is kept, and nothing waits while the graph is captured
+    t.on(0x5000, 35, capturing=True)
+    c._bind_stream()
+    third = c._ws
+    c._need_workspace(400)
+    assert c._kept == (third,) and t.synchronised == 1 and third.recorded == []
+
+
 def test_no_context_is_refused():
     from paper_2512_21450_b200 import build
     from paper_2512_21450_b200.binding import load_library
@@ -117,6 +160,41 @@ def test_two_streams_through_the_module_level_functions():
         for a, b in zip(outs, want[i]):
             assert torch.equal(a, b), i
     assert rl.default_context(0).last_device_status()[0] == 0
+
+
+@pytest.mark.gpu
+def test_memory_of_a_replaced_workspace_is_not_handed_out_while_another_stream_uses_it():
+    from paper_2512_21450_b200 import Context
+    c = Context(0)
+    try:
+        H, W, y, m = _data(500, 512, 6000, 5)
+        side, done = torch.cuda.Stream(), torch.cuda.Event()
+        other = Context(0)                            # loads the kernels, which may wait for the device
+        with torch.cuda.stream(side):
+            for n in (100, 500):
+                other.rl_cross_entropy_fwd_bwd(H[:n], W, y[:n], m[:n])
+        other.close()
+        want = c.rl_cross_entropy_fwd_bwd(H[:100], W, y[:100], m[:100])
+        address, size = c._ws.data_ptr(), c._ws.numel()
+        cached = [torch.empty(size, dtype=torch.uint8, device=DEV).fill_(0) for _ in range(4)]
+        del cached
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(1_000_000_000)          # half a second
+            got = c.rl_cross_entropy_fwd_bwd(H[:100], W, y[:100], m[:100])
+            assert c._ws.data_ptr() == address
+            c.rl_cross_entropy_fwd_bwd(H, W, y, m)
+            assert c._ws.numel() > size
+            done.record()
+        assert not done.query()
+        others = [torch.empty(size, dtype=torch.uint8, device=DEV) for _ in range(5)]
+        assert address not in [x.data_ptr() for x in others]
+        for x in others:
+            x.fill_(0xff)
+        torch.cuda.synchronize()
+        assert all(torch.equal(got[k], want[k]) for k in want)
+    finally:
+        c.close()
 
 
 @pytest.mark.gpu
