@@ -16,9 +16,10 @@ class _FusedHeadLoss(torch.autograd.Function):
     def forward(ctx, H, W, tokens, old_logp, ref_logp, adv, mask, eps_low, eps_high, beta, ent_coef, token_weight,
                 agg_mode, sequence_level, seq_offsets):
         lib = default_context(W.device.index or 0)
-        out = lib.rl_policy_loss_fwd_bwd(H.detach(), W.detach(), tokens, old_logp, ref_logp, adv, mask, eps_low,
-                                         eps_high, beta, ent_coef=ent_coef, token_weight=token_weight,
-                                         agg_mode=agg_mode, sequence_level=sequence_level, seq_offsets=seq_offsets)
+        with lib.turn:
+            out = lib.rl_policy_loss_fwd_bwd(H.detach(), W.detach(), tokens, old_logp, ref_logp, adv, mask, eps_low,
+                                             eps_high, beta, ent_coef=ent_coef, token_weight=token_weight,
+                                             agg_mode=agg_mode, sequence_level=sequence_level, seq_offsets=seq_offsets)
         ctx.save_for_backward(out["dH"], out["dW"])
         ctx.mark_non_differentiable(out["logp"], out["entropy"], out["metrics"])
         return out["loss"].reshape(()).clone(), out["logp"], out["entropy"], out["metrics"]
@@ -46,9 +47,10 @@ class _FusedCrossEntropy(torch.autograd.Function):
     @staticmethod
     def forward(ctx, H, W, targets, mask, label_smoothing, z_coef, token_weight, token_count, want_dH, want_dW):
         lib = default_context(W.device.index or 0)
-        out = lib.rl_cross_entropy_fwd_bwd(H.detach(), W.detach(), targets, mask, label_smoothing=label_smoothing, z_coef=z_coef,
-                                           token_weight=token_weight, token_count=token_count, want_dH=want_dH, want_dW=want_dW,
-                                           dW_bf16=True)
+        with lib.turn:
+            out = lib.rl_cross_entropy_fwd_bwd(H.detach(), W.detach(), targets, mask, label_smoothing=label_smoothing, z_coef=z_coef,
+                                               token_weight=token_weight, token_count=token_count, want_dH=want_dH, want_dW=want_dW,
+                                               dW_bf16=True)
         ctx.save_for_backward(out.get("dH"), out.get("dW"))
         ctx.mark_non_differentiable(out["logp"])
         return out["loss"].reshape(()).clone(), out["logp"]

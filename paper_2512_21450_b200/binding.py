@@ -12,6 +12,7 @@ import ctypes
 import importlib.util
 import os
 import sys
+import threading
 import warnings
 from ctypes import POINTER, byref, c_char_p, c_float, c_int, c_int32, c_int64, c_size_t, c_void_p
 
@@ -280,7 +281,8 @@ class Context:
 
     Calls run on torch's current stream.  Where that is another one than at the call before, they still follow one another, since they share
     the workspace: streams that are to work side by side have a context each.  Replays of graphs are calls that the context does not
-    see: whoever replays orders them with each other and with the context's other calls.  One thread at a time."""
+    see: whoever replays orders them with each other and with the context's other calls.  One thread at a time: `turn` is a lock for callers that share a context (it may be taken
+    again by the thread that has it)."""
 
     _captured, _kept = False, ()   # whether calls were captured with the present workspace; earlier ones that calls were captured with
     _foreign = False               # whether the stream that calls ran on last belongs to somebody else than torch
@@ -297,6 +299,7 @@ class Context:
         self._ws_key = None
         self._slot_busy = [False, False]
         self._stream = None
+        self.turn = threading.RLock()
 
     def close(self):
         if self.handle:
@@ -958,45 +961,67 @@ def debug_schedule(n_valid, rows_cap, k_len, n_tiles, n_range=1, n_fastest=0, m_
 
 
 _default_ctx = {}
+_default_lock = threading.Lock()
 
 
 def default_context(device=0):
-    if device not in _default_ctx:
-        _default_ctx[device] = Context(device)
-    return _default_ctx[device]
+    """The context of the device that the module-level functions and `autograd` share.  They take `turn` for the length of a call, so any
+    thread may call them; whoever calls the context itself while other threads do so takes it too."""
+    ctx = _default_ctx.get(device)
+    if ctx is None:
+        with _default_lock:
+            ctx = _default_ctx.get(device)
+            if ctx is None:
+                ctx = _default_ctx[device] = Context(device)
+    return ctx
 
 
 def rl_grpo_advantages(rewards, group_size, **kw):
-    return default_context(rewards.device.index or 0).rl_grpo_advantages(rewards, group_size, **kw)
+    ctx = default_context(rewards.device.index or 0)
+    with ctx.turn:
+        return ctx.rl_grpo_advantages(rewards, group_size, **kw)
 
 
 def rl_token_logprobs(H, W, tokens, mask=None):
-    return default_context(H.device.index or 0).rl_token_logprobs(H, W, tokens, mask)
+    ctx = default_context(H.device.index or 0)
+    with ctx.turn:
+        return ctx.rl_token_logprobs(H, W, tokens, mask)
 
 
 def rl_policy_loss_fwd_bwd(H, W, tokens, old_logp, ref_logp, adv, mask, eps_low, eps_high, beta, **kw):
-    return default_context(W.device.index or 0).rl_policy_loss_fwd_bwd(
-        H, W, tokens, old_logp, ref_logp, adv, mask, eps_low, eps_high, beta, **kw)
+    ctx = default_context(W.device.index or 0)
+    with ctx.turn:
+        return ctx.rl_policy_loss_fwd_bwd(H, W, tokens, old_logp, ref_logp, adv, mask, eps_low, eps_high, beta, **kw)
 
 
 def rl_cross_entropy_fwd_bwd(H, W, targets, mask=None, **kw):
-    return default_context(W.device.index or 0).rl_cross_entropy_fwd_bwd(H, W, targets, mask, **kw)
+    ctx = default_context(W.device.index or 0)
+    with ctx.turn:
+        return ctx.rl_cross_entropy_fwd_bwd(H, W, targets, mask, **kw)
 
 
 def rl_quantize_rows(X, **kw):
-    return default_context(X.device.index or 0).rl_quantize_rows(X, **kw)
+    ctx = default_context(X.device.index or 0)
+    with ctx.turn:
+        return ctx.rl_quantize_rows(X, **kw)
 
 
 def rl_int8_matmul(A, a_scale, Wq, w_scale, **kw):
-    return default_context(Wq.device.index or 0).rl_int8_matmul(A, a_scale, Wq, w_scale, **kw)
+    ctx = default_context(Wq.device.index or 0)
+    with ctx.turn:
+        return ctx.rl_int8_matmul(A, a_scale, Wq, w_scale, **kw)
 
 
 def rl_int8_linear(X, Wq, w_scale, **kw):
-    return default_context(Wq.device.index or 0).rl_int8_linear(X, Wq, w_scale, **kw)
+    ctx = default_context(Wq.device.index or 0)
+    with ctx.turn:
+        return ctx.rl_int8_linear(X, Wq, w_scale, **kw)
 
 
 def rl_token_logprobs_int8(H, Wq, w_scale, tokens, mask=None):
-    return default_context(Wq.device.index or 0).rl_token_logprobs_int8(H, Wq, w_scale, tokens, mask)
+    ctx = default_context(Wq.device.index or 0)
+    with ctx.turn:
+        return ctx.rl_token_logprobs_int8(H, Wq, w_scale, tokens, mask)
 
 
 def rl_token_logprobs_static(H, W, tokens, mask, logp, entropy=None, lse=None, dev_status=None):

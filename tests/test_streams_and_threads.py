@@ -1,4 +1,7 @@
-"""Calls of one context from several streams: its workspace and device block are one, so they follow one another."""
+"""Calls of one context from several streams and threads: its workspace and device block are one, so they follow one another."""
+import threading
+import time
+
 import pytest
 import torch
 
@@ -115,6 +118,58 @@ def test_every_stream_that_used_a_workspace_is_waited_for_before_its_memory_goes
     assert c._kept == (third,) and t.synchronised == 1 and third.recorded == []
 
 
+def _in_threads(work, n):
+    raised = []
+
+    def run(i):
+        try:
+            work(i)
+        except BaseException as e:
+            raised.append(e)
+    threads = [threading.Thread(target=run, args=(i,)) for i in range(n)]
+    for x in threads:
+        x.start()
+    for x in threads:
+        x.join(60)
+    assert not raised and not any(x.is_alive() for x in threads), raised
+
+
+def test_threads_take_turns_on_the_shared_context(monkeypatch):
+    """A call of the module-level functions binds a stream, then a workspace, then launches, with the interpreter's lock given up in between."""
+    import paper_2512_21450_b200 as rl
+    from paper_2512_21450_b200 import autograd, binding
+
+    made, inside, overlaps, seen = [], [], [], []
+
+    class Shared:
+        def __init__(self, device):
+            time.sleep(0.05)
+            made.append(device)
+            self.turn = threading.RLock()
+
+        def __getattr__(self, name):
+            def call(*args, **kw):
+                inside.append(name)
+                time.sleep(0.002)
+                if len(inside) > 1:
+                    overlaps.append(list(inside))
+                inside.remove(name)
+                seen.append(name)
+                z = torch.zeros(1)
+                return dict(loss=z, dH=z, dW=z, logp=z.clone(), entropy=z.clone(), metrics=z.clone())
+            return call
+    monkeypatch.setattr(binding, "Context", Shared)
+    monkeypatch.setattr(binding, "_default_ctx", {})
+    x = torch.zeros(1)
+    calls = [lambda: rl.rl_grpo_advantages(x, 1), lambda: rl.rl_token_logprobs(x, x, x),
+             lambda: rl.rl_policy_loss_fwd_bwd(x, x, x, x, x, x, x, 0.2, 0.2, 0.0), lambda: rl.rl_cross_entropy_fwd_bwd(x, x, x),
+             lambda: rl.rl_quantize_rows(x), lambda: rl.rl_int8_matmul(x, x, x, x), lambda: rl.rl_int8_linear(x, x, x),
+             lambda: rl.rl_token_logprobs_int8(x, x, x, x), lambda: autograd.fused_cross_entropy(x, x, x),
+             lambda: autograd.fused_grpo_head_loss(x, x, x, x, x, x, x)]
+    _in_threads(lambda i: [calls[(i + k) % len(calls)]() for k in range(len(calls))], 6)
+    assert made == [0] and not overlaps and len(seen) == 6 * len(calls)
+
+
 def test_no_context_is_refused():
     from paper_2512_21450_b200 import build
     from paper_2512_21450_b200.binding import load_library
@@ -160,6 +215,35 @@ def test_two_streams_through_the_module_level_functions():
         for a, b in zip(outs, want[i]):
             assert torch.equal(a, b), i
     assert rl.default_context(0).last_device_status()[0] == 0
+
+
+@pytest.mark.gpu
+def test_threads_through_the_module_level_functions():
+    """Several threads, a stream and sizes of its own each, on the context that they share."""
+    import paper_2512_21450_b200 as rl
+    from paper_2512_21450_b200.autograd import fused_cross_entropy
+    data = [_data(*s, i) for i, s in enumerate([(300, 512, 9000), (40, 1024, 5000), (700, 256, 3000)])]
+
+    def calls(H, W, y, m):
+        Wq, ws = rl.rl_quantize_rows(W)
+        out = rl.rl_cross_entropy_fwd_bwd(H, W, y, m, label_smoothing=0.1)
+        h = H.clone().requires_grad_()
+        fused_cross_entropy(h, W, y, m)[0].backward()
+        return [out[k] for k in ("loss", "logp", "dH", "dW")] + list(rl.rl_token_logprobs_int8(H, Wq, ws, y, m)) + [rl.rl_int8_linear(H, Wq, ws), h.grad]
+    want = [calls(*x) for x in data]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(i):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            for turn in range(8):
+                got = calls(*data[i])
+                stream.synchronize()
+                if not all(torch.equal(a, b) for a, b in zip(got, want[i])):
+                    wrong.append((i, turn))
+    _in_threads(work, 3)
+    assert not wrong and rl.default_context(0).last_device_status()[0] == 0
 
 
 @pytest.mark.gpu
