@@ -2,11 +2,14 @@
 
 The library computes the loss and both gradients in one call, so the autograd Function does all
 the work in `forward` and only scales the stored gradients by the incoming gradient in
-`backward`.  Marshalling only: the arithmetic is the C ABI's.
+`backward`.  Marshalling only: the arithmetic is the C ABI's.  The stored gradients are numbers, not functions of H and W:
+differentiating them again raises.
 """
 from __future__ import annotations
 
 import torch
+
+from torch.autograd.function import once_differentiable
 
 from .binding import default_context
 
@@ -25,6 +28,7 @@ class _FusedHeadLoss(torch.autograd.Function):
         return out["loss"].reshape(()).clone(), out["logp"], out["entropy"], out["metrics"]
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, g_loss, *_):
         dH, dW = ctx.saved_tensors
         gH = (dH.float() * g_loss).to(dH.dtype) if ctx.needs_input_grad[0] else None
@@ -56,6 +60,7 @@ class _FusedCrossEntropy(torch.autograd.Function):
         return out["loss"].reshape(()).clone(), out["logp"]
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, g_loss, *_):
         dH, dW = ctx.saved_tensors
         return (None if dH is None else dH * g_loss, None if dW is None else dW * g_loss) + (None,) * 8
