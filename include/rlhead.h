@@ -452,24 +452,26 @@ rl_status rl_token_logprobs_static(void* cuda_stream, const void* H, int64_t ldH
  * stage, a supervised term beside the policy loss, or (dH and dW NULL) an evaluation.  With z = W h_t, lse_t = log sum_j exp z_tj:
  *   l_t  = (1 - e) (lse_t - z_ty) + e (lse_t - mean_j z_tj) + z_coef lse_t^2,   e = label_smoothing,   loss = sum_t w_t l_t,
  *   dloss/dz_tj = w_t [(1 + 2 z_coef lse_t) p_tj - (1 - e) 1[j = y_t] - e / V],
- * w_t = mask_t / sum(mask) unless opts say otherwise.  targets[T] int32 (rows with mask 0 are left out whatever they hold, and get 0
+ * w_t = mask_t / sum(mask) unless opts say otherwise (NULL: all of them zero).  targets[T] int32 (rows with mask 0 are left out whatever they hold, and get 0
  * in every output); everything else as in rl_policy_loss_fwd_bwd.  dH or dW may be NULL: a gradient nobody needs (a frozen trunk or a
  * frozen head) is not formed.  dW is [V,d] fp32 or bf16, dH [T,d] bf16 or fp32.  Logits exist for one bounded slab of rows at a time,
  * in fp32 (rl_set_slab_limits).  Workspace: rl_workspace_bytes_ce (a bf16 dW of a call of several slabs is summed in fp32 there);
  * with neither gradient rl_workspace_bytes_logprobs.
  * H may be stored in 8 bits (rl_quantize_rows): opts->H_scale[T] then holds the scales, H points to int8_t, ldH counts bytes and is a
  * multiple of 16; the rows stand for bf16(H_scale[t] * H[t,k]) and dH is the gradient of those.
- * Errors: label_smoothing outside [0, 1), z_coef negative or not finite, an unknown type, a bf16 dW with accumulate_dW or with a
+ * The type of a dW has to be named, since its buffer is the caller's: a dW without opts, or with a struct that ends before dW_dtype, is
+ * refused; 0 is RL_BF16, so a struct of zeros asks for a bf16 dW (and accumulate_dW needs RL_FP32).
+ * Errors: label_smoothing outside [0, 1), z_coef negative or not finite, an unknown type, a dW of no named type, a bf16 dW with accumulate_dW or with a
  * rl_dw_slab_hook set, NULL loss, W or (T > 0) H, targets -> RL_ERR_INVALID_ARG; shape / alignment / workspace as above. */
 typedef enum { RL_BF16 = 0, RL_FP32 = 1, RL_FP16 = 2 } rl_dtype;
 typedef struct {
-  size_t struct_size;         /* sizeof(rl_ce_opts); the rest zero unless set (dW_dtype: RL_FP32)  */
+  size_t struct_size;         /* sizeof(rl_ce_opts); the rest zero unless set                  */
   float label_smoothing;      /* e, in [0, 1)                                                  */
   float z_coef;               /* >= 0                                                          */
   const float* token_weight;  /* [T] or NULL: w_t = mask_t token_weight[t]                     */
   const int64_t* token_count; /* device scalar or NULL: divisor of the token mean              */
   int accumulate_dW;          /* non-zero: dW += gradient (fp32 dW)                            */
-  int dH_dtype, dW_dtype;     /* RL_BF16 or RL_FP32                                            */
+  int dH_dtype, dW_dtype;     /* RL_BF16 (0) or RL_FP32                                        */
   const float* H_scale;       /* [T] or NULL: H is stored in 8 bits                            */
   float* logp_out;            /* [T] or NULL: z_ty - lse_t                                     */
   float* lse_out;             /* [T] or NULL                                                   */

@@ -1892,7 +1892,8 @@ rl_status rl_cross_entropy_fwd_bwd(rl_ctx* c, const void* H, int64_t ldH, const 
   if (!c) return RL_ERR_INVALID_ARG;
   rl_ce_opts o;
   memset(&o, 0, sizeof(o));
-  o.dW_dtype = RL_FP32;
+  // nothing is presumed about a buffer of the caller's: half of an fp32 dW would be written as bf16, or past a bf16 one
+  if (dW && (!opts || opts->struct_size < offsetof(rl_ce_opts, dW_dtype) + sizeof(o.dW_dtype))) return RL_ERR_INVALID_ARG;
   if (opts) {
     if (opts->struct_size < offsetof(rl_ce_opts, token_weight) || opts->struct_size > sizeof(o)) return RL_ERR_INVALID_ARG;
     memcpy(&o, opts, opts->struct_size);
