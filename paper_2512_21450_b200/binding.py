@@ -317,14 +317,21 @@ class Context:
         # the raw handle of torch's current stream, without building a Stream object for every call; the context keeps the
         # one it was given last
         stream = torch._C._cuda_getCurrentRawStream(self.device.index)
-        if torch._C._cuda_isCurrentStreamCapturing():
+        if self._capturing():
             self._captured = True
         if stream != self._stream:
             self._change_stream(stream)
 
+    def _capturing(self):
+        """Whether the context's device's current stream is being captured; torch answers for the current device's."""
+        if torch._C._cuda_getDevice() == self.device.index:
+            return bool(torch._C._cuda_isCurrentStreamCapturing())
+        with torch.cuda.device(self.device):
+            return bool(torch._C._cuda_isCurrentStreamCapturing())
+
     def _change_stream(self, stream):
         now = torch.cuda.current_stream(self.device)
-        capturing = torch._C._cuda_isCurrentStreamCapturing()
+        capturing = self._capturing()
         if self._stream is None or (self._foreign and capturing):
             _check(self.lib.rl_set_stream(self.handle, stream), "rl_set_stream")
         elif self._foreign:
@@ -344,7 +351,7 @@ class Context:
                 self._kept += (self._ws,)
             elif self._foreign and self._ws is not None:
                 torch.cuda.synchronize(self.device)   # what is recorded on such a stream may outlive it
-            self._captured = bool(torch._C._cuda_isCurrentStreamCapturing())
+            self._captured = self._capturing()
             self._ws = None
             self._ws = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=self.device)
         _check(self.lib.rl_set_workspace(self.handle, _ptr(self._ws), self._ws.numel()), "rl_set_workspace")

@@ -12,7 +12,8 @@ class _Torch:
     """What Context asks torch for, without a device: the current stream's handle, its id and whether it is captured."""
 
     def __init__(self, monkeypatch):
-        self.handle, self.id, self.capturing, self.synchronised = 0, 0, False, 0
+        self.handle, self.id, self.capturing, self.synchronised, self.device = 0, 0, False, 0, 0
+        monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: self.device, raising=False)
         monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: self.handle, raising=False)
         monkeypatch.setattr(torch._C, "_cuda_isCurrentStreamCapturing", lambda: self.capturing, raising=False)
         monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: type("Stream", (), dict(stream_id=self.id, cuda_stream=self.handle)))
@@ -116,6 +117,34 @@ def test_every_stream_that_used_a_workspace_is_waited_for_before_its_memory_goes
     third = c._ws
     c._need_workspace(400)
     assert c._kept == (third,) and t.synchronised == 1 and third.recorded == []
+
+
+def test_a_capture_on_another_device_than_the_current_one_is_seen(monkeypatch):
+    """A workspace that a graph of device 0 writes to is kept, whatever device is current at the call."""
+    import contextlib
+    t, c = _Torch(monkeypatch), _context()
+    monkeypatch.setattr(torch, "empty", lambda n, **kw: _Workspace(n))
+    captured = {0: False, 1: False}
+    monkeypatch.setattr(torch._C, "_cuda_isCurrentStreamCapturing", lambda: captured[t.device])
+
+    @contextlib.contextmanager
+    def device(d):
+        before, t.device = t.device, d.index
+        yield
+        t.device = before
+    monkeypatch.setattr(torch.cuda, "device", device)
+    c._bind_stream()
+    c._need_workspace(100)
+    first = c._ws
+    t.device, captured[0] = 1, True
+    c._bind_stream()
+    c._need_workspace(200)
+    assert c._kept == (first,) and t.device == 1
+    captured[0], captured[1], second = False, True, c._ws     # and not what another device captures
+    c._captured = False
+    c._bind_stream()
+    c._need_workspace(300)
+    assert c._kept == (first,) and c._ws is not second
 
 
 def _in_threads(work, n):
