@@ -459,6 +459,10 @@ rl_status rl_token_logprobs_static(void* cuda_stream, const void* H, int64_t ldH
  * with neither gradient rl_workspace_bytes_logprobs.
  * H may be stored in 8 bits (rl_quantize_rows): opts->H_scale[T] then holds the scales, H points to int8_t, ldH counts bytes and is a
  * multiple of 16; the rows stand for bf16(H_scale[t] * H[t,k]) and dH is the gradient of those.
+ * Numbers: the products add up in fp32 on the tensor cores, which cut off what does not fit (logp and loss are off by 1e-6 to 3e-6 of their
+ * size at d = 2048 to 3584); the gradient of the logits is rounded to bf16 before the products that dH and dW are.  The token mean's weight
+ * and 1 - e are multiplied in behind those, in fp32; a token_weight is part of what is rounded, so the same weight in every row
+ * (1/n, say) is the same rounding in every row: for a mean over another count use token_count.
  * The type of a dW has to be named, since its buffer is the caller's: a dW without opts, or with a struct that ends before dW_dtype, is
  * refused; 0 is RL_BF16, so a struct of zeros asks for a bf16 dW (and accumulate_dW needs RL_FP32).
  * Errors: label_smoothing outside [0, 1), z_coef negative or not finite, an unknown type, a dW of no named type, a bf16 dW with accumulate_dW or with a

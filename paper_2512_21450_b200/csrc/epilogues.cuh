@@ -22,7 +22,8 @@ __device__ __forceinline__ float ex2_approx(float x) {
 // Forward statistics (policy over the vocabulary, section 2.2): for its row and the vocabulary
 // range of the work unit, keeps the running maximum M, S = sum exp(z-M), A = sum exp(z-M) z and
 // the logit of the sampled token.  Logits never leave the chip; one float4 per (range, row) does.
-// SUM: A = sum z instead, for the cross entropy, whose smoothed labels ask for the mean logit and which needs no entropy.
+// SUM: A = sum z instead, for the cross entropy, whose smoothed labels ask for the mean logit and which needs no entropy.  In fp32, as S is:
+// a rounding of 2^-24 for every 32 columns, beside logits whose products are cut off as they add up.
 template <bool SUM>
 struct RowStatsOf {
   static constexpr bool kParts = false;

@@ -197,10 +197,12 @@ struct ColumnScales {
 // Eight epilogue warps in place of four up to these widths: the products take half the time that bf16's do, so the epilogue shows to
 // twice the width, less where it has a box to wait for.  8192 rows x 151936 words, four / eight, d = 512 / 1024 / 1536 / 2048 / 2560:
 // statistics 1209 / 1454 / 1728 / 1900 / 2155 us, 953 / 1207 / 1456 / 1846 / 2255; bf16 logits 972 / 1277 / 1591 / 1910 / 2283 us, 856 / 1262 /
-// 1682 / 2114 / 2486; fp32 logits 1211 / 1637 / 2113 / 2408 / 2835, 1080 / 1619 / 2087 / 2527 / 2966.
+// 1682 / 2114 / 2486; fp32 logits 1211 / 1637 / 2113 / 2408 / 2835, 1080 / 1619 / 2087 / 2527 / 2966.  At d = 1024 eight take 1 to 5 % less time
+// (on another box bf16 1226 / 1187, fp16 1348 / 1283, fp32 1673 / 1592): the line for logits lies on the safe side, below it.
 constexpr int kEightWarpsStatsI8 = 2048;
 constexpr int kEightWarpsScale = 768;
-// Row by row (no TMA): 2048 rows x 50257 words, four / eight warps, bf16 227 / 171 us at d = 1024, 205 / 182 at 2048; fp32 192 / 216, 206 / 229.
+// Row by row (no TMA): 50257 words, four / eight warps, 2048 rows at d = 1024 bf16 136 / 135 us, fp16 137 / 135, fp32 163 / 182; 599 rows 80 / 66, 76 / 64,
+// 77 / 77; 2048 rows at d = 2048 171 / 178, 182 / 194, 225 / 252.
 template <int OUT>
 constexpr int kWarpsByRow = OUT == 1 ? 4 : 8;
 

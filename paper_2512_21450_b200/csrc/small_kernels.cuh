@@ -970,7 +970,8 @@ __global__ void __launch_bounds__(kLossThreads) combine_loss_kernel(const LossPa
       if (p.each_out) p.each_out[row] = each;
       // G is formed without the token mean's weight and 1 - smooth, which the gradients get in fp32 where they leave: the entry of
       // a target that is unlikely is then near -1, and not the same rounding of (1 - smooth) / n in every row.  dH of 12 thousand
-      // rows is off by 1.9e-3 that way (the rounding of the result alone: 1.7e-3), by 2.7e-3 with the weight in G
+      // rows is off by 1.9e-3 that way (the rounding of the result alone: 1.7e-3), by 2.7e-3 with the weight in G.  Weights of the
+      // caller's differ from row to row and stay in G: the same weight in many rows is the same rounding in all of them
       const float u = p.token_weight ? tw : 1.f;
       p.cp_c[i] = u * fmaf(2.f * p.z_coef, lse, 1.f) / (1.f - p.smooth);
       p.ce_c[i] = u;
