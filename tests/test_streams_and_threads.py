@@ -293,7 +293,7 @@ def test_memory_of_a_replaced_workspace_is_not_handed_out_while_another_stream_u
         del cached
         torch.cuda.synchronize()
         with torch.cuda.stream(side):
-            torch.cuda._sleep(1_000_000_000)          # half a second
+            torch.cuda._sleep(3_000_000_000)          # more than a second
             got = c.rl_cross_entropy_fwd_bwd(H[:100], W, y[:100], m[:100])
             assert c._ws.data_ptr() == address
             c.rl_cross_entropy_fwd_bwd(H, W, y, m)
